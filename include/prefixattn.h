@@ -380,13 +380,84 @@ int pa_gather_kv(const void* kv_pool, const int32_t* slots, int64_t n, int Hkv, 
                  int64_t num_slots, int dtype, void* k_out, void* v_out, void* stream);
 
 /* ---------------------------------------------------------------------------------
+ * Latent attention: models whose cache is one latent vector a token, shared by all query heads.
+ *
+ * A cached token is a row (c, r) of R latent and P rotary values instead of K and V of every KV
+ * head.  The tree, the matcher and the page allocator above serve it unchanged (slots are slots);
+ * the pool, the scatter and the attention have forms of their own.  R in {256, 512}, P = 64, any
+ * number of heads H.  dtype as elsewhere: PA_F32, PA_BF16, or PA_BF16_KV8 = bf16 tensors with c in
+ * 8 bits in the pool.
+ *
+ * Pool (rows by slot; pages do not show in it): PA_F32 and PA_BF16, R + P elements a row.
+ * PA_BF16_KV8: a row is R one-byte codes (4 exponent bits, 3 mantissa bits, bias 7, no infinities,
+ * largest 448) followed by the P rotary values in bf16; behind the last row lies one int8 exponent
+ * k per slot, c = code * 2^k with the smallest k for which max|c| * 2^-k <= 448 (in [-100, 119], 0
+ * for a row of zeros), rounded to nearest, ties to even, saturating: the format of the fp8 KV pool.
+ * Values have to be finite there.
+ * --------------------------------------------------------------------------------- */
+
+/* Bytes of a pool of num_slots rows; 0 if the arguments are invalid. */
+size_t pa_latent_pool_bytes(int64_t num_slots, int R, int P, int dtype);
+
+/* pool[new_slots[t]] = c_ext[t] (c_ext [T, R + P]), quantised on the way with PA_BF16_KV8.
+ * new_slots int32 [T], pairwise distinct (the caller's responsibility: of two rows for one slot an
+ * unspecified mixture is left) and in [0, num_slots); a slot outside the pool is skipped. */
+int pa_append_latent(void* latent_pool, const int32_t* new_slots, const void* c_ext, int64_t T, int R, int P,
+                     int64_t num_slots, int dtype, void* stream);
+
+/* c_out[i] = pool[slots[i]] as stored (decoded with PA_BF16_KV8), c_out [n, R + P]; slots may repeat;
+ * rows of slots outside the pool are left as they were. */
+int pa_gather_latent(const void* latent_pool, const int32_t* slots, int64_t n, int R, int P, int64_t num_slots,
+                     int dtype, void* c_out, void* stream);
+
+/* Bytes of workspace pa_latent_attention needs for these arguments or smaller B, T and max_kv_len;
+ * 0 if they are invalid. */
+size_t pa_latent_workspace_bytes(int B, int64_t T, int64_t max_kv_len, int H, int R, int P, int dtype);
+
+/* Attention of new tokens over cached latent rows, absorbed form: the queries come multiplied with
+ * the key up-projection already, the output still has to be multiplied with the value up-projection.
+ * With P_r = prefix_len[r], extend row i of request r and head h see the rows (c_j, r_j) of the P_r
+ * cached tokens at slot_idx[slot_offsets[r] + j] and of extend tokens 0..i:
+ *     out[e0 + i, h, :] = sum_j softmax_j(scale * <q_ext[e0 + i, h, :], (c_j, r_j)>) c_j
+ * q_ext [T, H, R + P]   c_ext [T, R + P], the rows of the extend tokens (as given: not quantised)
+ * out   [T, H, R]       latent_pool as written by pa_append_latent with the same R, P, num_slots, dtype
+ * The other arguments, what happens to slots outside the pool, to requests without extend tokens and
+ * to a batch on the device larger than T says (pa_extend_status, bf16) are as for pa_extend_attention;
+ * scale has to be positive and finite.  workspace: at least pa_latent_workspace_bytes(...), 256-byte
+ * aligned, whatever it holds; calls that overlap in time must not share one.  B at most 65,536. */
+int pa_latent_attention(const void* q_ext, const void* c_ext, const void* latent_pool, const int32_t* slot_idx,
+                        const int32_t* slot_offsets, const int32_t* prefix_len, const int32_t* ext_len,
+                        const int32_t* ext_offsets, int B, int64_t T, int64_t max_kv_len, int H, int R, int P,
+                        int64_t num_slots, int dtype, float scale, void* out, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+/* The same for pa_latent_attention_expanded (it holds expanded keys and values of a group of heads). */
+size_t pa_latent_expanded_workspace_bytes(int B, int64_t T, int64_t max_kv_len, int H, int R, int P, int N,
+                                          int64_t num_slots, int dtype);
+
+/* Expanded form: every head has keys (W_k[h] c_j, r_j) and values W_v[h] c_j,
+ *     out[e0 + i, h, :] = sum_j softmax_j(scale * (<q_n, W_k[h] c_j> + <q_r, r_j>)) W_v[h] c_j,  (q_n, q_r) = q_ext[e0 + i, h, :]
+ * q_ext [T, H, N + P]   w_k, w_v [H, N, R]   out [T, H, N]   N in {64, 128}
+ * Less arithmetic than the absorbed form from some hundred new tokens behind a cached one on: a row of
+ * q costs 2 (2 N + P) operations per key and head instead of 2 (2 R + P), against 4 N R once per
+ * distinct cached slot and head.  The other arguments as above. */
+int pa_latent_attention_expanded(const void* q_ext, const void* c_ext, const void* w_k, const void* w_v,
+                                 const void* latent_pool, const int32_t* slot_idx, const int32_t* slot_offsets,
+                                 const int32_t* prefix_len, const int32_t* ext_len, const int32_t* ext_offsets,
+                                 int B, int64_t T, int64_t max_kv_len, int H, int R, int P, int N,
+                                 int64_t num_slots, int dtype, float scale, void* out, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------
  * Per-kernel timing for benchmarks (not part of the method).  While enabled, every kernel
  * the library launches is bracketed by two HIP events on its stream (this creates events on
  * first use, so do not enable it under stream capture).  pa_profile_enable(1) clears the
  * records and starts recording, pa_profile_enable(0) stops.  pa_profile_read waits for the
  * recorded events and returns the summed device time (ms) and the number of launches of one
  * kernel, named "match_prefixes", "extend_plan", "extend_attention", "extend_merge",
- * "extend_attention_f32", "append_kv", "gather_kv", "calib_copy" or "calib_mfma".  At most 65536 launches are recorded.
+ * "extend_attention_f32", "append_kv", "gather_kv", "append_latent", "gather_latent", "latent_attention",
+ * "latent_merge", "latent_attention_f32", "latent_expand", "latent_attention_expanded", "calib_copy" or
+ * "calib_mfma".  At most 65536 launches are recorded.
  * --------------------------------------------------------------------------------- */
 int pa_profile_enable(int on);
 int pa_profile_read(const char* kernel, double* total_ms, int64_t* launches);

@@ -65,6 +65,13 @@ _SIGS = {
     "pa_extend_set_row_sharing": (_i, [_i]),
     "pa_append_kv": (_i, [_vp, _vp, _vp, _vp, _i64, _i, _i, _i, _i64, _i, _vp]),
     "pa_gather_kv": (_i, [_vp, _vp, _i64, _i, _i, _i, _i64, _i, _vp, _vp, _vp]),
+    "pa_latent_pool_bytes": (_sz, [_i64, _i, _i, _i]),
+    "pa_append_latent": (_i, [_vp, _vp, _vp, _i64, _i, _i, _i64, _i, _vp]),
+    "pa_gather_latent": (_i, [_vp, _vp, _i64, _i, _i, _i64, _i, _vp, _vp]),
+    "pa_latent_workspace_bytes": (_sz, [_i, _i64, _i64, _i, _i, _i, _i]),
+    "pa_latent_attention": (_i, [_vp] * 8 + [_i, _i64, _i64, _i, _i, _i, _i64, _i, _f, _vp, _vp, _sz, _vp]),
+    "pa_latent_expanded_workspace_bytes": (_sz, [_i, _i64, _i64, _i, _i, _i, _i, _i64, _i]),
+    "pa_latent_attention_expanded": (_i, [_vp] * 10 + [_i, _i64, _i64, _i, _i, _i, _i, _i64, _i, _f, _vp, _vp, _sz, _vp]),
     "pa_profile_enable": (_i, [_i]),
     "pa_profile_read": (_i, [C.c_char_p, C.POINTER(C.c_double), C.POINTER(_i64)]),
     "pa_profile_clock": (_i, [_vp, _i, C.POINTER(C.c_double)]),
@@ -375,6 +382,33 @@ def gather_kv(kv_pool: torch.Tensor, slots: torch.Tensor, *, Hkv: int, D: int, d
     _check(_lib.pa_gather_kv(_ptr(kv_pool), _ptr(slots), n, Hkv, D, page_size, num_slots, _code(dtype, kv8), _ptr(k),
                              _ptr(v), _stream(stream)), "pa_gather_kv")
     return k, v
+
+
+def latent_pool_bytes(num_slots: int, latent_dim: int, rope_dim: int, dtype: torch.dtype, kv8: bool = False) -> int:
+    n = int(_lib.pa_latent_pool_bytes(num_slots, latent_dim, rope_dim, _code(dtype, kv8)))
+    if n == 0:
+        raise ValueError("pa_latent_pool_bytes: invalid arguments")
+    return n
+
+
+def latent_workspace_bytes(B: int, T: int, max_kv_len: int, H: int, latent_dim: int, rope_dim: int, dtype: torch.dtype) -> int:
+    n = int(_lib.pa_latent_workspace_bytes(B, T, max_kv_len, H, latent_dim, rope_dim, _DTYPES[dtype]))
+    if n == 0:
+        raise ValueError("pa_latent_workspace_bytes: invalid arguments")
+    return n
+
+
+def latent_expanded_workspace_bytes(B: int, T: int, max_kv_len: int, H: int, latent_dim: int, rope_dim: int, N: int, num_slots: int,
+                                    dtype: torch.dtype) -> int:
+    n = int(_lib.pa_latent_expanded_workspace_bytes(B, T, max_kv_len, H, latent_dim, rope_dim, N, num_slots, _DTYPES[dtype]))
+    if n == 0:
+        raise ValueError("pa_latent_expanded_workspace_bytes: invalid arguments")
+    return n
+
+
+# Latent attention (one row of latent_dim + rope_dim values a token, shared by all heads): marshalled in native code as well.
+append_latent, gather_latent = _calls.append_latent, _calls.gather_latent
+latent_attention, latent_attention_expanded = _calls.latent_attention, _calls.latent_attention_expanded
 
 
 def profile_enable(on: bool, clock_probe: bool = False) -> None:

@@ -7,6 +7,7 @@
 #include <Python.h>
 #include <ATen/ATen.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
@@ -336,6 +337,263 @@ PyObject* append_kv(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject
     CALLS_CATCH
 }
 
+// ---- latent attention ----
+
+// A contiguous device tensor of rows of width R + P; *R from `rope`.  False with an exception set.
+bool latent_rows_of(const at::Tensor& t, const char* name, long long rope, int* R) {
+    if (!t.is_cuda() || !t.is_contiguous()) {
+        PyErr_Format(PyExc_TypeError, "%s must be a contiguous CUDA tensor", name);
+        return false;
+    }
+    if (t.dim() != 2 || rope < 0 || t.size(1) <= rope || t.size(1) > INT32_MAX) {
+        PyErr_Format(PyExc_ValueError, "%s must have the shape [rows, latent_dim + rope_dim]", name);
+        return false;
+    }
+    *R = static_cast<int>(t.size(1) - rope);
+    return true;
+}
+
+bool latent_pool_ok(const at::Tensor& pool, const at::Tensor& like, long long num_slots, int R, long long P, int dtype) {
+    if (!pool.is_cuda() || !pool.is_contiguous() || pool.device() != like.device()) {
+        PyErr_SetString(PyExc_TypeError, "latent_pool must be a contiguous CUDA tensor on the device of the other tensors");
+        return false;
+    }
+    const size_t need = P > INT32_MAX ? 0 : pa_latent_pool_bytes(num_slots, R, static_cast<int>(P), dtype);
+    if (need == 0) PyErr_SetString(PyExc_ValueError, "pa_latent_pool_bytes: invalid arguments");
+    else if (pool.nbytes() < need) PyErr_SetString(PyExc_ValueError, "latent_pool smaller than pa_latent_pool_bytes");
+    return need != 0 && pool.nbytes() >= need;
+}
+
+bool number_of(PyObject* o, const char* name, long long* out) {
+    if (!o) {
+        PyErr_Format(PyExc_TypeError, "%s must be an integer", name);
+        return false;
+    }
+    *out = PyLong_AsLongLong(o);
+    return !(*out == -1 && PyErr_Occurred());
+}
+
+// Kernels run on the device of the call's tensors, whatever the current one is.
+struct OnDeviceOf {
+    int before = 0, dev;
+    bool other;
+    explicit OnDeviceOf(const at::Tensor& t) : dev(t.device().index()) {
+        other = hipGetDevice(&before) == hipSuccess && before != dev && hipSetDevice(dev) == hipSuccess;
+    }
+    ~OnDeviceOf() { if (other) (void)hipSetDevice(before); }
+    OnDeviceOf(const OnDeviceOf&) = delete;
+    OnDeviceOf& operator=(const OnDeviceOf&) = delete;
+};
+
+// The stream of a latent call: as stream_of, but torch's current stream on the device of its tensors.
+bool stream_on(PyObject* o, const at::Tensor& t, void** out) {
+    if (o) return stream_of(o, out);
+    *out = static_cast<void*>(c10::hip::getCurrentHIPStream(t.device().index()).stream());
+    return true;
+}
+
+// append_latent(latent_pool, new_slots, c_ext, *, rope_dim, num_slots, stream=None, kv8=False)
+PyObject* append_latent(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+    static const char* const names[] = {"latent_pool", "new_slots", "c_ext", "rope_dim", "num_slots", "stream", "kv8"};
+    PyObject* a[7];
+    if (!parse_args("append_latent", names, 3, 3, args, nargs, kwnames, a)) return nullptr;
+    CALLS_TRY
+    const at::Tensor* t[3];
+    for (int i = 0; i < 3; ++i)
+        if (!(t[i] = tensor_of(a[i], names[i]))) return nullptr;
+    const at::Tensor &pool = *t[0], &slots = *t[1], &c = *t[2];
+    long long rope = 0, num_slots = 0;
+    int dtype = 0, R = 0;
+    if (!device_int32(slots, "new_slots") || !dtype_of(c, a[6], &dtype) || !number_of(a[3], "rope_dim", &rope) ||
+        !number_of(a[4], "num_slots", &num_slots) || !latent_rows_of(c, "c_ext", rope, &R) || !latent_pool_ok(pool, c, num_slots, R, rope, dtype))
+        return nullptr;
+    if (slots.numel() != c.size(0) || slots.device() != c.device()) {
+        PyErr_SetString(PyExc_ValueError, "append_latent: new_slots and c_ext disagree");
+        return nullptr;
+    }
+    void* stream = nullptr;
+    if (!stream_on(a[5], c, &stream)) return nullptr;
+    int rc = PA_OK;
+    {
+        const WithoutGil released;
+        const OnDeviceOf here(c);
+        rc = pa_append_latent(pool.data_ptr(), static_cast<const int32_t*>(slots.const_data_ptr()), c.const_data_ptr(), c.size(0), R,
+                              static_cast<int>(rope), num_slots, dtype, stream);
+    }
+    if (rc != PA_OK) return raise_code(rc, "pa_append_latent");
+    Py_RETURN_NONE;
+    CALLS_CATCH
+}
+
+// gather_latent(latent_pool, slots, *, latent_dim, rope_dim, dtype, num_slots, out=None, stream=None, kv8=False)
+PyObject* gather_latent(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+    static const char* const names[] = {"latent_pool", "slots", "latent_dim", "rope_dim", "dtype", "num_slots", "out", "stream", "kv8"};
+    PyObject* a[9];
+    if (!parse_args("gather_latent", names, 2, 2, args, nargs, kwnames, a)) return nullptr;
+    CALLS_TRY
+    const at::Tensor *pool = tensor_of(a[0], "latent_pool"), *slots = pool ? tensor_of(a[1], "slots") : nullptr;
+    if (!slots || !device_int32(*slots, "slots")) return nullptr;
+    long long R = 0, rope = 0, num_slots = 0;
+    if (!number_of(a[2], "latent_dim", &R) || !number_of(a[3], "rope_dim", &rope) || !number_of(a[5], "num_slots", &num_slots)) return nullptr;
+    if (!a[4] || !THPDtype_Check(a[4])) {
+        PyErr_SetString(PyExc_TypeError, "dtype must be a torch dtype");
+        return nullptr;
+    }
+    if (R <= 0 || R > INT32_MAX / 2 || rope < 0 || rope > INT32_MAX / 2) {
+        PyErr_SetString(PyExc_ValueError, "pa_latent_pool_bytes: invalid arguments");
+        return nullptr;
+    }
+    const at::TensorOptions options = slots->options().dtype(reinterpret_cast<THPDtype*>(a[4])->scalar_type);
+    void* stream = nullptr;
+    if (!stream_on(a[7], *slots, &stream)) return nullptr;
+    at::Tensor made;
+    const at::Tensor* out = nullptr;
+    if (a[6]) {
+        if (!(out = tensor_of(a[6], "out"))) return nullptr;
+        if (out->scalar_type() != reinterpret_cast<THPDtype*>(a[4])->scalar_type || !out->is_contiguous() || out->device() != slots->device() ||
+            out->dim() != 2 || out->size(0) != slots->numel() || out->size(1) != R + rope) {
+            PyErr_SetString(PyExc_ValueError, "bad out tensor");
+            return nullptr;
+        }
+    } else {
+        const AllocateOn streams(stream, *slots);
+        out = &(made = streams.given(at::empty({slots->numel(), R + rope}, options)));
+    }
+    int dtype = 0;
+    if (!dtype_of(*out, a[8], &dtype) || !latent_pool_ok(*pool, *slots, num_slots, static_cast<int>(R), rope, dtype)) return nullptr;
+    int rc = PA_OK;
+    {
+        const WithoutGil released;
+        const OnDeviceOf here(*slots);
+        rc = pa_gather_latent(pool->const_data_ptr(), static_cast<const int32_t*>(slots->const_data_ptr()), slots->numel(), static_cast<int>(R),
+                              static_cast<int>(rope), num_slots, dtype, out->data_ptr(), stream);
+    }
+    if (rc != PA_OK) return raise_code(rc, "pa_gather_latent");
+    return a[6] ? Py_NewRef(a[6]) : THPVariable_Wrap(made);
+    CALLS_CATCH
+}
+
+// Both forms of the attention.  kExpanded: w_k and w_v follow c_ext, and the rotary width comes from the shapes.
+template <bool kExpanded>
+PyObject* latent_call(PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
+    static const char* const fn = kExpanded ? "latent_attention_expanded" : "latent_attention";
+    static const char* const names_absorbed[] = {"q_ext", "c_ext", "latent_pool", "slot_idx", "slot_offsets", "prefix_len", "ext_len", "ext_offsets",
+                                                 "scale", "rope_dim", "num_slots", "max_kv_len", "out", "workspace", "stream", "kv8"};
+    static const char* const names_expanded[] = {"q_ext", "c_ext", "w_k", "w_v", "latent_pool", "slot_idx", "slot_offsets", "prefix_len", "ext_len",
+                                                 "ext_offsets", "scale", "num_slots", "max_kv_len", "out", "workspace", "stream", "kv8"};
+    constexpr int W = kExpanded ? 2 : 0, S = 8 + W;  // weights; index of scale
+    PyObject* a[kExpanded ? 17 : 16];
+    if constexpr (kExpanded) {
+        if (!parse_args(fn, names_expanded, S + 1, S + 1, args, nargs, kwnames, a)) return nullptr;
+    } else {
+        if (!parse_args(fn, names_absorbed, S + 1, S + 1, args, nargs, kwnames, a)) return nullptr;
+    }
+    const char* const* const names = kExpanded ? names_expanded : names_absorbed;
+    CALLS_TRY
+    const at::Tensor* t[S];
+    for (int i = 0; i < S; ++i)
+        if (!(t[i] = tensor_of(a[i], names[i]))) return nullptr;
+    const at::Tensor &q = *t[0], &c = *t[1], &pool = *t[2 + W], &prefix_len = *t[5 + W];
+    PyObject* const* const rest = a + S + (kExpanded ? 0 : 1);  // rest[1] = num_slots, and so on
+    int dtype = 0;
+    if (!dtype_of(q, rest[6], &dtype)) return nullptr;
+    for (int i = 0; i < 2 + W; ++i)
+        if (!t[i]->is_cuda() || !t[i]->is_contiguous() || t[i]->scalar_type() != q.scalar_type() || t[i]->device() != q.device()) {
+            PyErr_Format(PyExc_TypeError, "%s must be a contiguous CUDA tensor of dtype %s, on the device of q_ext", names[i], c10::toString(q.scalar_type()));
+            return nullptr;
+        }
+    long long rope = 0, num_slots = 0, max_kv_len = 0;
+    int N = 0, R = 0;
+    if constexpr (kExpanded) {
+        const at::Tensor &wk = *t[2], &wv = *t[3];
+        if (q.dim() != 3 || wk.dim() != 3 || wk.size(0) != q.size(1) || wv.sizes() != wk.sizes() || q.size(2) <= wk.size(1)) {
+            PyErr_SetString(PyExc_ValueError, "q_ext [T, H, N + P], w_k and w_v [H, N, R] disagree");
+            return nullptr;
+        }
+        N = static_cast<int>(wk.size(1));
+        rope = q.size(2) - N;
+    } else if (!number_of(a[S + 1], "rope_dim", &rope)) {
+        return nullptr;
+    }
+    if (!latent_rows_of(c, "c_ext", rope, &R)) return nullptr;
+    if (q.dim() != 3 || q.size(0) != c.size(0) || (!kExpanded && q.size(2) != c.size(1)) || (kExpanded && t[2]->size(2) != R)) {
+        PyErr_SetString(PyExc_ValueError, "q_ext and c_ext disagree");
+        return nullptr;
+    }
+    const int64_t T = q.size(0), B = prefix_len.numel();
+    const int H = static_cast<int>(q.size(1));
+    for (int i = 3 + W; i < S; ++i) {
+        if (!device_int32(*t[i], names[i])) return nullptr;
+        if (t[i]->device() != q.device()) {
+            PyErr_Format(PyExc_TypeError, "%s must be on the device of q_ext", names[i]);
+            return nullptr;
+        }
+    }
+    if (B > INT32_MAX || t[4 + W]->numel() != B + 1 || t[7 + W]->numel() != B + 1 || t[6 + W]->numel() != B) {
+        PyErr_SetString(PyExc_ValueError, "per-request arrays disagree on B");
+        return nullptr;
+    }
+    if (!a[S]) {
+        PyErr_SetString(PyExc_TypeError, "scale must be a number");
+        return nullptr;
+    }
+    const double scale = PyFloat_AsDouble(a[S]);
+    if (scale == -1.0 && PyErr_Occurred()) return nullptr;
+    if (!number_of(rest[1], "num_slots", &num_slots) || !number_of(rest[2], "max_kv_len", &max_kv_len)) return nullptr;
+    if (!latent_pool_ok(pool, q, num_slots, R, rope, dtype)) return nullptr;
+    void* stream = nullptr;
+    if (!stream_on(rest[5], q, &stream)) return nullptr;
+    const size_t need = kExpanded ? pa_latent_expanded_workspace_bytes(static_cast<int>(B), T, max_kv_len, H, R, static_cast<int>(rope), N, num_slots, dtype)
+                                  : pa_latent_workspace_bytes(static_cast<int>(B), T, max_kv_len, H, R, static_cast<int>(rope), dtype);
+    if (need == 0) {
+        PyErr_Format(PyExc_ValueError, "%s: invalid arguments", kExpanded ? "pa_latent_expanded_workspace_bytes" : "pa_latent_workspace_bytes");
+        return nullptr;
+    }
+    const int64_t width = kExpanded ? N : R;
+    at::Tensor made_out, made_ws;
+    const at::Tensor *out = nullptr, *ws = nullptr;
+    if (rest[3]) {
+        if (!(out = tensor_of(rest[3], "out"))) return nullptr;
+        if (out->dim() != 3 || out->size(0) != T || out->size(1) != H || out->size(2) != width || out->scalar_type() != q.scalar_type() ||
+            !out->is_contiguous() || out->device() != q.device()) {
+            PyErr_SetString(PyExc_ValueError, "bad out tensor");
+            return nullptr;
+        }
+    }
+    if (rest[4]) {
+        if (!(ws = tensor_of(rest[4], "workspace"))) return nullptr;
+        if (!ws->is_contiguous() || ws->device() != q.device()) {
+            PyErr_SetString(PyExc_ValueError, "workspace must be a contiguous tensor on the device of q_ext");
+            return nullptr;
+        }
+    }
+    if (!out || !ws) {
+        const AllocateOn streams(stream, q);
+        if (!out) out = &(made_out = streams.given(at::empty({T, H, width}, q.options())));
+        if (!ws) ws = &(made_ws = at::empty({static_cast<int64_t>(need)}, q.options().dtype(at::kByte)));
+    }
+    auto i32 = [&](int i) { return static_cast<const int32_t*>(t[i + W]->const_data_ptr()); };
+    int rc = PA_OK;
+    {
+        const WithoutGil released;
+        const OnDeviceOf here(q);
+        if constexpr (kExpanded)
+            rc = pa_latent_attention_expanded(q.const_data_ptr(), c.const_data_ptr(), t[2]->const_data_ptr(), t[3]->const_data_ptr(),
+                                              pool.const_data_ptr(), i32(3), i32(4), i32(5), i32(6), i32(7), static_cast<int>(B), T, max_kv_len, H, R,
+                                              static_cast<int>(rope), N, num_slots, dtype, static_cast<float>(scale), out->data_ptr(),
+                                              ws->data_ptr(), ws->nbytes(), stream);
+        else
+            rc = pa_latent_attention(q.const_data_ptr(), c.const_data_ptr(), pool.const_data_ptr(), i32(3), i32(4), i32(5), i32(6), i32(7),
+                                     static_cast<int>(B), T, max_kv_len, H, R, static_cast<int>(rope), num_slots, dtype,
+                                     static_cast<float>(scale), out->data_ptr(), ws->data_ptr(), ws->nbytes(), stream);
+    }
+    if (rc != PA_OK) return raise_code(rc, kExpanded ? "pa_latent_attention_expanded" : "pa_latent_attention");
+    return rest[3] ? Py_NewRef(rest[3]) : THPVariable_Wrap(made_out);
+    CALLS_CATCH
+}
+PyObject* latent_attention(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) { return latent_call<false>(args, nargs, kwnames); }
+PyObject* latent_attention_expanded(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) { return latent_call<true>(args, nargs, kwnames); }
+
 // tree_admit(tree, tokens, now) -> (n_cached, new_slots, handle), or None where tokens is no contiguous int32 vector in host
 // memory or now no Python integer: nothing is done then, and the caller converts tokens or goes through ctypes, which takes (and
 // refuses) all other types.  Native because a serving loop makes this call once per request: marshalled through ctypes and torch
@@ -388,6 +646,20 @@ PyMethodDef g_methods[] = {
     {"append_kv", PA_FAST(append_kv),
      "append_kv($module, /, kv_pool, new_slots, k_ext, v_ext, *, page_size, num_slots, stream=None, kv8=False)\n--\n\n"
      "pool[new_slots[t]] = (k_ext[t], v_ext[t]).  Asynchronous on the stream."},
+    {"append_latent", PA_FAST(append_latent),
+     "append_latent($module, /, latent_pool, new_slots, c_ext, *, rope_dim, num_slots, stream=None, kv8=False)\n--\n\n"
+     "pool[new_slots[t]] = c_ext[t], rows [T, latent_dim + rope_dim].  Asynchronous on the stream."},
+    {"gather_latent", PA_FAST(gather_latent),
+     "gather_latent($module, /, latent_pool, slots, *, latent_dim, rope_dim, dtype, num_slots, out=None, stream=None, kv8=False)\n--\n\n"
+     "-> the rows of these slots as stored, [n, latent_dim + rope_dim].  Asynchronous on the stream."},
+    {"latent_attention", PA_FAST(latent_attention),
+     "latent_attention($module, /, q_ext, c_ext, latent_pool, slot_idx, slot_offsets, prefix_len, ext_len, ext_offsets, scale, *, "
+     "rope_dim, num_slots, max_kv_len, out=None, workspace=None, stream=None, kv8=False)\n--\n\n"
+     "Absorbed form: q_ext [T,H,R+P], c_ext [T,R+P] -> out [T,H,R].  Asynchronous on the stream."},
+    {"latent_attention_expanded", PA_FAST(latent_attention_expanded),
+     "latent_attention_expanded($module, /, q_ext, c_ext, w_k, w_v, latent_pool, slot_idx, slot_offsets, prefix_len, ext_len, ext_offsets, "
+     "scale, *, num_slots, max_kv_len, out=None, workspace=None, stream=None, kv8=False)\n--\n\n"
+     "Expanded form: q_ext [T,H,N+P], c_ext [T,R+P], w_k and w_v [H,N,R] -> out [T,H,N].  Asynchronous on the stream."},
     {"tree_admit", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(tree_admit)), METH_FASTCALL,
      "tree_admit($module, tree, tokens, now, /)\n--\n\n-> (n_cached, new_slots, handle), or None if tokens or now is of another type than the usual one."},
     {"setup", setup, METH_O, "setup($module, error_class, /)\n--\n\nThe exception class error codes are raised as."},

@@ -11,7 +11,10 @@ namespace pa {
 
 static const char* const kKernelNames[kProfKernels] = {"match_prefixes", "extend_plan",        "extend_attention",
                                                        "extend_merge",   "extend_attention_f32", "append_kv",
-                                                       "gather_kv",      "calib_copy",           "calib_mfma"};
+                                                       "gather_kv",      "calib_copy",           "calib_mfma",
+                                                       "append_latent",  "gather_latent",      "latent_attention",
+                                                       "latent_merge",   "latent_attention_f32", "latent_expand",
+                                                       "latent_attention_expanded"};
 
 struct ProfRecord {
     hipEvent_t start, stop;
