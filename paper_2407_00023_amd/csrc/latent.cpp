@@ -8,6 +8,9 @@ int latent_attention_rows(const void* q, const LatentBatch& b, int H, int R, int
 int latent_expanded_rows(const void* q, const LatentBatch& b, const void* w_k, const void* w_v, int H, int R, int N, int dtype, float scale,
                          void* out, void* scratch, hipStream_t stream);
 size_t latent_expanded_rows_bytes(int64_t T, int H, int R);
+size_t latent_workspace_bytes_bf16(int B, int64_t T, int64_t max_kv_len, int H, int R);
+int latent_attention_bf16(const void* q, const LatentBatch& b, int64_t max_kv_len, int H, int R, bool kv8, float scale, void* out, void* workspace,
+                          hipStream_t stream);
 
 constexpr int kMaxRequests = 65536;
 
@@ -42,7 +45,8 @@ static int check(const char* fn, const void* q, const LatentBatch& b, int64_t ma
 }  // namespace pa
 
 extern "C" size_t pa_latent_workspace_bytes(int B, int64_t T, int64_t max_kv_len, int H, int R, int P, int dtype) {
-    return pa::sizes_ok(B, T, max_kv_len, H, R, P, dtype) ? 256 : 0;
+    if (!pa::sizes_ok(B, T, max_kv_len, H, R, P, dtype)) return 0;
+    return dtype == PA_F32 ? 256 : pa::latent_workspace_bytes_bf16(B, T, max_kv_len, H, R);  // (fp32 needs none; 0 means invalid)
 }
 
 extern "C" int pa_latent_attention(const void* q_ext, const void* c_ext, const void* latent_pool, const int32_t* slot_idx,
@@ -55,6 +59,8 @@ extern "C" int pa_latent_attention(const void* q_ext, const void* c_ext, const v
     if (const int rc = pa::check("pa_latent_attention", q_ext, b, max_kv_len, H, R, P, dtype, scale, out, workspace, workspace_bytes, need, &nothing))
         return rc;
     if (nothing) return PA_OK;
+    if (dtype != PA_F32)
+        return pa::latent_attention_bf16(q_ext, b, max_kv_len, H, R, dtype == PA_BF16_KV8, scale, out, workspace, static_cast<hipStream_t>(stream));
     return pa::latent_attention_rows(q_ext, b, H, R, dtype, scale, out, static_cast<hipStream_t>(stream));
 }
 

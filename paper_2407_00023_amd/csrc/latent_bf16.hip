@@ -1,0 +1,595 @@
+// Latent attention on the bf16 matrix cores, absorbed form (MFMA 16x16x32, fp32 accumulation), gfx950.
+//
+// A row (c, r) of R latent and kRope rotary values is the key of all H query heads, and c their value:
+//     S = Q K^T (R + kRope deep),  P = 2^(c S - m),  O = P C (R columns),  out = O / sum P.
+// Per cached row 2 (2 R + kRope) H operations for 2 (R + kRope) bytes: with 16 heads memory bounds it, with 128 the matrix cores about as
+// much as memory, from two new tokens on the matrix cores.
+//
+// Tiles.  The rows of q of a request (token, head) are one axis, so that a tile of M rows reads every cached row once for all of its heads and
+// tokens.  Four waves, M = 128 or 32.  What decides the layout is the width of the output: 512 fp32 columns for 128 rows are 256 KB, half of a
+// compute unit's registers, so one workgroup is resident, a wave per SIMD with 512 registers, and the two products are split differently:
+//   scores: a wave computes 32 rows x 32 keys (M = 32: 16 x 16), its rows of Q, all R + kRope of them, in registers;
+//   output: a wave computes all M rows x a quarter of the columns, so that a fragment of C read from LDS is multiplied with eight blocks of
+//           rows; the probabilities go through LDS in between.  (A wave with the output of its own 32 rows would read every fragment of C for
+//           two products only: 68 KB of LDS reads per wave and step instead of 52, and LDS, not the matrix cores, would be the bound.)
+// Scores are computed transposed (S^T = K Q^T): a lane holds one row of q per block and four keys, the output as O^T = C^T P^T, C^T by the
+// transposing LDS read, so that row maxima and sums are per lane and O's rows too.
+//
+// Pipeline.  A step is 32 keys.  In one interval between two barriers a wave computes the scores and probabilities of step i + 1 and the output of
+// step i, and the rows of step i + 3 are on their way from memory straight into LDS, those of step i + 2 landing.  The running maximum of a
+// row only moves when a score outgrows it by kGrow: a wave that sees one sets a flag, and behind the barrier all waves settle on new maxima together
+// (settle()); a probability may reach 2^kGrow until then, which fp32 and bf16 hold as exactly as 1.
+//
+// LDS is swizzled in pieces of 16 bytes (swz()) so that reading 16 bytes down 16 rows and the transposing reads of 8 bytes across 8 rows are both
+// free of bank conflicts; direct loads write 1 KB of consecutive LDS, so the swizzle is applied to the address in memory.
+//
+// 8-bit pool: codes land in a buffer of their own and are turned into bf16 rows by the wave that loaded them, one step before they are used.
+#include <hip/hip_bf16.h>
+
+#include <type_traits>
+
+#include "fp8_rows.h"
+#include "latent_work.h"
+#include "wave_ops.h"
+
+namespace pa {
+
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kGrow = 40.f;  // log2 units
+
+__device__ const uint4 g_zero_row[128] = {};  // stands for keys behind the last one of a tile
+
+// XOR of the 16-byte piece of a latent row in LDS, by the row's number within 16; and of its rotary part (8 pieces)
+__device__ __forceinline__ int swz(int row) { return ((row & 1) << 3) | ((row & 2) << 1) | ((row & 8) >> 2) | ((row >> 2) & 1); }
+__device__ __forceinline__ int swz_rope(int row) { return (row >> 1) & 7; }
+
+template <int R, int M, bool KV8>
+struct LatentShape {
+    static constexpr int kLatRow = 2 * R, kLat = kStep * kLatRow;       // bytes of a latent row and of a step's
+    static constexpr int kLatSlots = KV8 ? 3 : 4, kRopeSlots = 3, kRopeStep = kStep * 2 * kRope;
+    static constexpr int kCodes = KV8 ? kStep * R : 0;
+    static constexpr int kProb = M * kStep * 2;
+    static constexpr int kRopeAt = kLatSlots * kLat, kCodesAt = kRopeAt + kRopeSlots * kRopeStep, kProbAt = kCodesAt + 2 * kCodes,
+                         kMaxAt = kProbAt + 2 * kProb, kRedAt = kMaxAt + 4 * M, kFlagAt = kRedAt + 8 * M, kSlotsAt = kFlagAt + 16,
+                         kExpAt = kSlotsAt + 4 * 2 * 256, kBytes = kExpAt + (KV8 ? 4 * 2 * 32 : 0);
+    static_assert(kBytes <= 160 * 1024, "LDS");
+};
+
+template <int R, int M, bool KV8>
+__global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat16* __restrict__ q_ext, LatentBatch b, LatentSplit split, float scale_log2e,
+                                                             __hip_bfloat16* __restrict__ out, LatentParts parts) {
+    using X = LatentShape<R, M, KV8>;
+    constexpr int L = R + kRope, KS = R / 32, KSR = kRope / 32;    // k-slices of the latent and the rotary part
+    constexpr int RW = M >= 64 ? 2 : 1, KW = M == 128 ? 2 : 1;    // blocks of 16 rows and of 16 keys of a wave's scores
+    constexpr int KG = M == 128 ? 1 : 2;                           // waves that share a row's scores
+    constexpr int RB = M / 16, NB = R / 64;                        // blocks of the output: rows, and 16 columns each of the wave's quarter
+    constexpr int RPL = 512 / R;                                   // latent rows of a 1 KB load
+    constexpr int PROW = KV8 ? R + 2 * kRope : 2 * L;              // bytes of a pool row
+    constexpr int kLoads = KV8 ? 8 * R / 1024 + 2 : 8 / RPL + 1;   // loads per wave of a step whose rows are all in the pool
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g4 = lane >> 4;
+    int wl = 0, at_work = 0;
+    LatentPlace at, end;
+    bool over = false;
+    const bool any = latent_share(b, split, blockIdx.x, reinterpret_cast<LatentScratch*>(smem), &wl, &at_work, &at, &end, &over);
+    if (blockIdx.x == 0 && tid == 0) {
+        parts.hdr[3] = over;
+        parts.hdr[6] = at_work;
+    }
+    if (!any) return;
+
+    const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem));
+    auto* const lds = (__attribute__((address_space(3))) unsigned char*)smem;
+    auto* const s_max = reinterpret_cast<float*>(smem + X::kMaxAt);
+    auto* const s_red = reinterpret_cast<float*>(smem + X::kRedAt);  // [KG][M]
+    auto* const s_flag = reinterpret_cast<int*>(smem + X::kFlagAt);
+    auto* const s_slots = reinterpret_cast<int*>(smem + X::kSlotsAt) + wave * 128;
+
+    // the wave's part of the scores
+    const int wrow = M == 128 ? 32 * wave : 16 * RW * (wave & 1), wkey = M == 128 ? 0 : 16 * (wave >> 1), kgroup = M == 128 ? 0 : wave >> 1;
+    // LDS read addresses: K fragments (16 rows from wkey on, piece 4 s + g4), by s mod 4; rotary; C^T fragments; probabilities
+    unsigned k_at[4], r_at[KSR], v_at;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) k_at[s] = (wkey + n) * X::kLatRow + 16 * ((4 * s + g4) ^ swz(n));
+#pragma unroll
+    for (int s = 0; s < KSR; ++s) r_at[s] = X::kRopeAt + (wkey + n) * 2 * kRope + 16 * ((4 * s + g4) ^ swz_rope(n));
+    {
+        const int row = 8 * g4 + (n >> 2);  // and 4 more
+        const int piece = (16 * NB * wave >> 3) + ((n & 3) >> 1);
+        v_at = row * X::kLatRow + 16 * (piece ^ swz(row & 15)) + 8 * (n & 1);
+    }
+    const unsigned p_rd = X::kProbAt + n * 64 + 16 * (g4 ^ (n >> 2));
+
+    bool used[2] = {false, false};  // partial results left in this workgroup's two slots
+    while (!(at.r == end.r && at.tile == end.tile && at.k == end.k)) {
+        bool unused = false;
+        LatentRequest req = latent_request(b, split, at.r, &unused);
+        req.P = __builtin_amdgcn_readfirstlane(req.P);
+        req.rows = __builtin_amdgcn_readfirstlane(req.rows);
+        req.tiles = __builtin_amdgcn_readfirstlane(req.tiles);
+        if (at.tile >= req.tiles) {
+            if (++at.r >= b.B) break;
+            at.tile = at.k = 0;
+            continue;
+        }
+        const int H = split.rpt, P = req.P, row0 = at.tile * M, rows_here = min(M, req.rows - row0);
+        const int64_t e0 = __builtin_amdgcn_readfirstlane(b.ext_offsets[at.r]);
+        const int32_t* __restrict__ slots = b.slot_idx + __builtin_amdgcn_readfirstlane(b.slot_offsets[at.r]);
+        const int key_end = latent_keys(split, req, at.tile), all_steps = (key_end + kStep - 1) / kStep;
+        const int k0 = at.k, k1 = at.r == end.r && at.tile == end.tile ? end.k : all_steps, steps = k1 - k0;
+        const int vis_min = P + row0 / H + 1;  // every row of the tile sees the keys before this one
+        const int64_t out_row0 = e0 * H + row0;
+
+        // ---- loads of a step: the wave's rows 8 wave .. + 7 ----
+        const unsigned char* const pool = static_cast<const unsigned char*>(b.pool);
+        const unsigned char* const c_rows = static_cast<const unsigned char*>(b.c_ext) + e0 * (2 * L);
+        auto row_address = [&](int j, int slot) -> uint64_t {
+            const unsigned s = min(static_cast<unsigned>(max(slot, 0)), static_cast<unsigned>(b.num_slots - 1));  // never outside the pool
+            const uint64_t in_pool = reinterpret_cast<uint64_t>(pool) + static_cast<uint64_t>(s) * PROW;
+            const uint64_t in_ext = reinterpret_cast<uint64_t>(c_rows) + static_cast<uint64_t>(max(j - P, 0)) * (2 * L);
+            return j < P ? in_pool : j < key_end ? in_ext : reinterpret_cast<uint64_t>(g_zero_row);
+        };
+        // slot ids of eight steps from step k0 + 8 blk on, lane: step lane / 8, row lane % 8
+        auto load_slots = [&](int blk) {
+            const int first = (k0 + 8 * blk) * kStep;
+            if (first < P) {
+                const int j = first + (lane >> 3) * kStep + 8 * wave + (lane & 7);
+                load_to_lds_4(slots + min(j, P - 1), lds0 + X::kSlotsAt + wave * 512 + (blk & 1) * 256);
+            }
+        };
+        auto issue = [&](int rel) {
+            const int j0 = (k0 + rel) * kStep + 8 * wave;
+            const int* const sl = s_slots + ((rel >> 3) & 1) * 64 + (rel & 7) * 8;
+            const unsigned lat = lds0 + (rel % X::kLatSlots) * X::kLat + 8 * wave * X::kLatRow, rope = lds0 + X::kRopeAt + (rel % X::kRopeSlots) * X::kRopeStep + 8 * wave * 2 * kRope;
+            if constexpr (!KV8 && RPL == 1) {
+                const uint64_t a = row_address(j0 + (lane & 7), sl[lane & 7]);
+                const unsigned lo = static_cast<unsigned>(a), hi = static_cast<unsigned>(a >> 32);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    // (readlane gives a signed word: it must not be extended by its sign)
+                    const uint64_t base = static_cast<unsigned>(__builtin_amdgcn_readlane(lo, i)) | static_cast<uint64_t>(static_cast<unsigned>(__builtin_amdgcn_readlane(hi, i))) << 32;
+                    load_to_lds_16(reinterpret_cast<const void*>(base), 16u * (lane ^ swz((8 * wave + i) & 15)), lat + i * X::kLatRow);
+                }
+            } else if constexpr (!KV8) {
+#pragma unroll
+                for (int i = 0; i < 8 / RPL; ++i) {
+                    const int row = i * RPL + lane / (64 / RPL);
+                    load_to_lds_16(reinterpret_cast<const unsigned char*>(row_address(j0 + row, sl[row])) + 16 * ((lane & (64 / RPL - 1)) ^ swz((8 * wave + row) & 15)),
+                                   lat + i * 1024);
+                }
+            }
+            if constexpr (KV8) {
+                const unsigned char* const exps = pool + static_cast<uint64_t>(b.num_slots) * PROW;
+#pragma unroll
+                for (int i = 0; i < 8 * R / 1024; ++i) {
+                    const int row = i * (1024 / R) + lane / (R / 16);
+                    if (j0 + row < P)
+                        load_to_lds_16(reinterpret_cast<const unsigned char*>(row_address(j0 + row, sl[row])) + 16 * (lane % (R / 16)),
+                                       lds0 + X::kCodesAt + (rel & 1) * X::kCodes + 8 * wave * R + i * 1024);
+                }
+                if (lane < 8 && j0 + lane < P)
+                    load_to_lds_1(exps + min(static_cast<unsigned>(max(sl[lane], 0)), static_cast<unsigned>(b.num_slots - 1)),
+                                  lds0 + X::kExpAt + wave * 64 + (rel & 1) * 32);
+            }
+            const int row = lane >> 3, j = j0 + row;
+            const uint64_t a = row_address(j, sl[row]);
+            load_to_lds_16(reinterpret_cast<const unsigned char*>(a) + (KV8 && j < P ? R : 2 * R) + 16 * ((lane & 7) ^ swz_rope((8 * wave + row) & 15)), rope);
+        };
+
+        // 8-bit pool.  All rows of a step are in the pool: its loads are kLoads, no row goes to its place in LDS directly.
+        auto pure = [&](int rel) { return !KV8 || (k0 + rel + 1) * kStep <= P; };
+        // rows that are bf16 in memory (extend tokens, and what stands for keys behind the last), to their place
+        auto issue_direct = [&](int rel) {
+            const int j0 = (k0 + rel) * kStep + 8 * wave;
+            const unsigned lat = lds0 + (rel % X::kLatSlots) * X::kLat + 8 * wave * X::kLatRow;
+#pragma unroll
+            for (int i = 0; i < 8 / RPL; ++i) {
+                const int row = i * RPL + lane / (64 / RPL);
+                if (j0 + row >= P)
+                    load_to_lds_16(reinterpret_cast<const unsigned char*>(row_address(j0 + row, 0)) + 16 * ((lane & (64 / RPL - 1)) ^ swz((8 * wave + row) & 15)),
+                                   lat + i * 1024);
+            }
+        };
+        // codes that landed, to bf16 rows (the wave's own)
+        auto convert = [&](int rel) {
+            const int j0 = (k0 + rel) * kStep + 8 * wave;
+            const unsigned from = X::kCodesAt + (rel & 1) * X::kCodes + 8 * wave * R, exps = X::kExpAt + wave * 64 + (rel & 1) * 32;
+            const unsigned to = (rel % X::kLatSlots) * X::kLat + 8 * wave * X::kLatRow;
+#pragma unroll
+            for (int i = 0; i < 8 / RPL; ++i) {
+                const int row = i * RPL + lane / (64 / RPL), piece = lane & (64 / RPL - 1);
+                if (j0 + row < P) {
+                    const u32x2 codes = *reinterpret_cast<__attribute__((address_space(3))) const u32x2*>(lds + from + row * R + 8 * piece);
+                    const float two_k = fp8_scale(*reinterpret_cast<__attribute__((address_space(3))) const signed char*>(lds + exps + 4 * row));
+                    const uint2 x = fp8_decode4(codes[0], two_k), y = fp8_decode4(codes[1], two_k);
+                    *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(lds + to + row * X::kLatRow + 16 * (piece ^ swz((8 * wave + row) & 15))) =
+                        u32x4{x.x, x.y, y.x, y.y};
+                }
+            }
+        };
+
+        // ---- the wave's rows of Q ----
+        bf16x8 q[RW][KS + KSR];
+        int vis[RW];
+        load_slots(0);
+#pragma unroll
+        for (int rb = 0; rb < RW; ++rb) {
+            const int row = min(wrow + 16 * rb + n, rows_here - 1);  // (rows behind the last repeat it)
+            vis[rb] = P + (row0 + row) / H + 1;
+            const uint4* const src = reinterpret_cast<const uint4*>(q_ext + (out_row0 + row) * L);
+#pragma unroll
+            for (int s = 0; s < KS + KSR; ++s) q[rb][s] = __builtin_bit_cast(bf16x8, src[4 * s + g4]);
+        }
+        float m[RW], l[RW];
+#pragma unroll
+        for (int rb = 0; rb < RW; ++rb) m[rb] = l[rb] = 0.f;
+        if (tid < 2) s_flag[tid] = -1;
+        wait_vm_all();
+        load_slots(1);
+        issue(0);
+        if (steps > 1) issue(1);
+        if (!KV8 && steps > 2) issue(2);
+        if (KV8) {
+            if (!pure(0)) issue_direct(0);
+            if (steps > 1 && !pure(1)) issue_direct(1);
+        }
+
+        // ---- the pieces of an interval ----
+        f32x4 sc[KW][RW];
+        auto scores = [&](int rel) {
+            const unsigned lat = (rel % X::kLatSlots) * X::kLat, rope = (rel % X::kRopeSlots) * X::kRopeStep;
+#pragma unroll
+            for (int kb = 0; kb < KW; ++kb)
+#pragma unroll
+                for (int rb = 0; rb < RW; ++rb) sc[kb][rb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int kb = 0; kb < KW; ++kb) {
+                    const bf16x8 kf = *reinterpret_cast<__attribute__((address_space(3))) const bf16x8*>(lds + (k_at[s & 3] + lat) + kb * 16 * X::kLatRow + (s >> 2) * 256);
+#pragma unroll
+                    for (int rb = 0; rb < RW; ++rb) sc[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[rb][s], sc[kb][rb], 0, 0, 0);
+                }
+#pragma unroll
+            for (int s = 0; s < KSR; ++s)
+#pragma unroll
+                for (int kb = 0; kb < KW; ++kb) {
+                    const bf16x8 kf = *reinterpret_cast<__attribute__((address_space(3))) const bf16x8*>(lds + (r_at[s] + rope) + kb * 16 * 2 * kRope);
+#pragma unroll
+                    for (int rb = 0; rb < RW; ++rb) sc[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[rb][KS + s], sc[kb][rb], 0, 0, 0);
+                }
+            const int j0 = (k0 + rel) * kStep;
+            if (j0 + kStep > vis_min) {
+#pragma unroll
+                for (int kb = 0; kb < KW; ++kb)
+#pragma unroll
+                    for (int rb = 0; rb < RW; ++rb)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (j0 + wkey + 16 * kb + 4 * g4 + i >= vis[rb]) sc[kb][rb][i] = -INFINITY;
+            }
+        };
+        // probabilities of the scores against the maxima as they stand, into buffer rel % 2; their sums
+        auto probabilities = [&](int rel) {
+            const unsigned to = X::kProbAt + (rel & 1) * X::kProb;
+#pragma unroll
+            for (int rb = 0; rb < RW; ++rb)
+#pragma unroll
+                for (int kb = 0; kb < KW; ++kb) {
+                    float p[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        p[i] = __builtin_amdgcn_exp2f(fmaf(sc[kb][rb][i], scale_log2e, -m[rb]));
+                        l[rb] += p[i];
+                    }
+                    const int piece = ((wkey + 16 * kb) >> 3) + (g4 >> 1);
+                    *reinterpret_cast<__attribute__((address_space(3))) u32x2*>(lds + to + (wrow + 16 * rb + n) * 64 + 16 * (piece ^ (n >> 2)) + 8 * (g4 & 1)) =
+                        u32x2{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3])};
+                }
+        };
+        auto largest = [&](int rb) {
+            float mx = sc[0][rb][0];
+#pragma unroll
+            for (int kb = 0; kb < KW; ++kb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[kb][rb][i]);
+            return mx * scale_log2e;
+        };
+        // All waves agree on new maxima of all rows, from the scores at hand (step rel), and write their probabilities.  What has been summed up
+        // against the old ones moves to the workgroup's scratch memory (flush), multiplied accordingly, and the accumulators begin anew.
+        auto settle = [&](int rel, bool first, auto flush) {
+#pragma unroll
+            for (int rb = 0; rb < RW; ++rb) {
+                const float mx = row_max(largest(rb));
+                if (g4 == 0) s_red[kgroup * M + wrow + 16 * rb + n] = mx;
+            }
+            lds_barrier();
+            auto new_max = [&](int row) {
+                float x = s_red[row];
+                if (KG == 2) x = fmaxf(x, s_red[M + row]);
+                if (first) return x == -INFINITY ? 0.f : x;  // (a row that sees no key here sees none behind it either)
+                return fmaxf(x, s_max[row]);
+            };
+            if (!first) flush([&](int row) { return __builtin_amdgcn_exp2f(s_max[row] - new_max(row)); });
+#pragma unroll
+            for (int rb = 0; rb < RW; ++rb) {
+                const float mn = new_max(wrow + 16 * rb + n);
+                l[rb] = first ? 0.f : l[rb] * __builtin_amdgcn_exp2f(m[rb] - mn);
+                m[rb] = mn;
+            }
+            const float mine = tid < M ? new_max(tid) : 0.f;
+            lds_barrier();
+            if (tid < M) s_max[tid] = mine;
+            probabilities(rel);
+            lds_barrier();
+        };
+        bool odd_seen = false;
+        auto output = [&](int rel, f32x4 (&o)[RB][NB], auto masked) __attribute__((always_inline)) {
+            const unsigned lat = (rel % X::kLatSlots) * X::kLat, prob = p_rd + (rel & 1) * X::kProb;
+            bf16x8 pf[RB];
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) pf[rb] = *reinterpret_cast<__attribute__((address_space(3))) const bf16x8*>(lds + prob + rb * 1024);
+#pragma unroll
+            for (int cb = 0; cb < NB; ++cb) {
+                const unsigned a = (v_at ^ (32 * cb)) + lat;
+                s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + a));
+                s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + (a ^ 16) + 4 * X::kLatRow));
+                s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                if constexpr (decltype(masked)::value) {
+                    // A key that some row does not see may hold an infinity or NaN, and 0 times that is NaN: such values are taken out of
+                    // the product here and given to the rows that see them at the end.
+                    bool odd = false;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if ((v[e] & 0x7F80) == 0x7F80) {
+                            odd = true;
+                            v[e] = 0;
+                        }
+                    if (__any(odd)) odd_seen = true;
+                }
+                const bf16x8 vf = __builtin_bit_cast(bf16x8, v);
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) o[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rb], o[rb][cb], 0, 0, 0);
+            }
+        };
+
+        // ---- the loop ----
+        if constexpr (KV8) {
+            wait_vm_all();
+            convert(0);
+            if (steps > 1) convert(1);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the codes are read: their buffer is free)
+            if (steps > 2) issue(2);
+            lds_barrier();
+            scores(0);
+        } else {
+            if (steps > 2) wait_vm<2 * kLoads>();
+            else if (steps > 1) wait_vm<kLoads>();
+            else wait_vm_all();
+            lds_barrier();
+            scores(0);
+            if (steps > 2) wait_vm<kLoads>();
+            else wait_vm_all();
+        }
+        settle(0, true, [](auto) {});
+        bool flushed = false;
+        float* const scratch = parts.o + (static_cast<size_t>(2 * split.n_wg + wl) * M + n) * R + 16 * NB * wave + 4 * g4;
+        for (int rel = 0; rel < steps;) {
+            f32x4 o[RB][NB];
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                for (int cb = 0; cb < NB; ++cb) o[rb][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
+            float l_before[RW];
+            bool grown = false;
+            while (!grown && rel < steps) {
+                if ((rel & 7) == 5) load_slots((rel + 3) / 8 + 1);
+                if (KV8 && rel + 2 < steps && !pure(rel + 2)) issue_direct(rel + 2);
+                if (rel + 3 < steps) issue(rel + 3);
+                if (rel + 1 < steps) {
+                    scores(rel + 1);
+#pragma unroll
+                    for (int rb = 0; rb < RW; ++rb) l_before[rb] = l[rb];
+                    probabilities(rel + 1);
+                    bool outgrown = false;
+#pragma unroll
+                    for (int rb = 0; rb < RW; ++rb) outgrown |= largest(rb) - m[rb] > kGrow;
+                    if (__any(outgrown) && lane == 0) s_flag[(rel + 1) & 1] = rel + 1;
+                }
+                if ((k0 + rel + 1) * kStep <= vis_min) output(rel, o, std::false_type{});
+                else output(rel, o, std::true_type{});
+                if (rel + 3 < steps && pure(rel + 3)) wait_vm<kLoads>();
+                else wait_vm_all();
+                if (KV8 && rel + 2 < steps) convert(rel + 2);
+                lds_barrier();
+                ++rel;
+                grown = rel < steps && __builtin_amdgcn_readfirstlane(s_flag[rel & 1]) == rel;
+            }
+            if (grown) {
+#pragma unroll
+                for (int rb = 0; rb < RW; ++rb) l[rb] = l_before[rb];  // (the probabilities are done again)
+                settle(rel, false, [&](auto alpha) {
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) {
+                        const float a = alpha(16 * rb + n);
+#pragma unroll
+                        for (int cb = 0; cb < NB; ++cb) {
+                            f32x4* const to = reinterpret_cast<f32x4*>(scratch + 16 * rb * R + 16 * cb);
+                            f32x4 x = o[rb][cb];
+                            if (flushed) x += *to;
+                            *to = x * a;
+                        }
+                    }
+                });
+                flushed = true;
+                continue;
+            }
+
+            // ---- the end of the tile, or of the workgroup's part of it ----
+#pragma unroll
+            for (int rb = 0; rb < RW; ++rb) {
+                const float sum = row_sum(l[rb]);
+                if (g4 == 0) s_red[kgroup * M + wrow + 16 * rb + n] = sum;
+            }
+            lds_barrier();
+            const bool head = k0 == 0, last = k1 == all_steps, whole = head && last;
+            auto row_total = [&](int row) { return KG == 2 ? s_red[row] + s_red[M + row] : s_red[row]; };
+            const int part = 2 * wl + (head ? 1 : 0);
+            if (!whole) {
+                used[head ? 1 : 0] = true;
+                if (tid == 0) parts.rec[part] = make_int4(static_cast<int>(out_row0), rows_here, (head ? kPartHead : 0) | (last ? kPartLast : 0), 0);
+                if (tid < rows_here) parts.ml[static_cast<size_t>(part) * M + tid] = make_float2(s_max[tid], row_total(tid));
+            }
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                const int row = 16 * rb + n;
+                if (row >= rows_here) continue;
+                const float inv = whole ? 1.f / row_total(row) : 1.f;
+                const int sees = P + (row0 + row) / H + 1;
+#pragma unroll
+                for (int cb = 0; cb < NB; ++cb) {
+                    f32x4 x = o[rb][cb];
+                    if (flushed) x += *reinterpret_cast<const f32x4*>(scratch + 16 * rb * R + 16 * cb);
+                    x *= inv;
+                    const int col = 16 * (NB * wave + cb) + 4 * g4;
+                    if (odd_seen) {
+                        // (a weight is positive: an infinity stays one, two of opposite sign and NaN give NaN)
+                        for (int j = max(vis_min & ~(kStep - 1), k0 * kStep); j < min(sees, k1 * kStep); ++j) {
+                            const bool cached = j < P;
+                            if (KV8 && cached) continue;  // (the 8-bit pool holds neither)
+                            const auto* const c4 = reinterpret_cast<const unsigned short*>(row_address(j, cached ? slots[j] : 0)) + col;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if ((c4[i] & 0x7F80) == 0x7F80) x[i] += __uint_as_float(static_cast<unsigned>(c4[i]) << 16);
+                        }
+                    }
+                    if (whole)
+                        *reinterpret_cast<uint2*>(out + (out_row0 + row) * R + col) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+                    else
+                        *reinterpret_cast<f32x4*>(parts.o + (static_cast<size_t>(part) * M + row) * R + col) = x;
+                }
+            }
+        }
+        lds_barrier();
+        ++at.tile;
+        at.k = 0;
+        if (k1 != all_steps) break;
+    }
+    if (tid < 2 && !used[tid]) parts.rec[2 * wl + tid] = make_int4(0, 0, 0, 0);
+}
+
+// The parts of a tile joined: workgroup (w, y) of the launch takes the tile that workgroup w of the attention began and did not finish, if there
+// is one, and kJoinRows of its rows.
+constexpr int kJoinRows = 4;
+template <int R>
+__global__ __launch_bounds__(256) void latent_merge_kernel(LatentParts parts, int M, __hip_bfloat16* __restrict__ out) {
+    constexpr int kCols = R / 4, kRowsAtOnce = 256 / kCols;  // threads of a row
+    __shared__ float s_w[512][kJoinRows];
+    const int w = blockIdx.x, n = parts.hdr[6];
+    if (w >= n) return;
+    const int4 rec = parts.rec[2 * w + 1];
+    const int row0 = blockIdx.y * kJoinRows;
+    if (!(rec.z & kPartHead) || row0 >= rec.y) return;
+    // parts: slot 2 w + 1, then 2 (w + 1), 2 (w + 2), ... up to the one that ends the tile
+    const int tid = threadIdx.x, lane = tid & 63;
+    int count = 1;
+    for (bool more = true; more;) {
+        const int i = w + count + lane;
+        const int flags = i < n ? parts.rec[2 * i].z : kPartLast;
+        const unsigned long long ends = __ballot(flags & kPartLast);
+        count += ends ? __builtin_ctzll(ends) + 1 : 64;
+        more = ends == 0;
+    }
+    auto slot = [&](int p) { return p == 0 ? 2 * w + 1 : 2 * (w + p); };
+    const int rows = min(kJoinRows, rec.y - row0);
+    // weights of the parts: 2^(their maximum - the largest) over the sum
+    if (tid < 64 * kJoinRows) {
+        const int row = tid >> 6;
+        if (row < rows) {
+            float mx = -INFINITY, sum = 0.f;
+            for (int p = lane; p < count; p += 64) {
+                const float2 ml = parts.ml[static_cast<size_t>(slot(p)) * M + row0 + row];
+                if (ml.y != 0.f) mx = fmaxf(mx, ml.x);  // (a part whose keys the row does not see says nothing)
+            }
+#pragma unroll
+            for (int off = 1; off < 64; off <<= 1) mx = fmaxf(mx, __shfl_xor(mx, off));
+            const float ref = mx == -INFINITY ? 0.f : mx;
+            for (int p = lane; p < count; p += 64) {
+                const float2 ml = parts.ml[static_cast<size_t>(slot(p)) * M + row0 + row];
+                const float a = ml.y != 0.f ? __builtin_amdgcn_exp2f(ml.x - ref) : 0.f;
+                s_w[p][row] = a;
+                sum += a * ml.y;
+            }
+#pragma unroll
+            for (int off = 1; off < 64; off <<= 1) sum += __shfl_xor(sum, off);
+            for (int p = lane; p < count; p += 64) s_w[p][row] /= sum;
+        }
+    }
+    __syncthreads();
+    const int c = tid % kCols;
+    for (int row = tid / kCols; row < rows; row += kRowsAtOnce) {
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int p = 0; p < count; ++p) {
+            const float a = s_w[p][row];
+            const float4 v = *reinterpret_cast<const float4*>(parts.o + (static_cast<size_t>(slot(p)) * M + row0 + row) * R + 4 * c);
+            if (a != 0.f) {
+                acc.x += a * v.x;
+                acc.y += a * v.y;
+                acc.z += a * v.z;
+                acc.w += a * v.w;
+            }
+        }
+        *reinterpret_cast<uint2*>(out + (static_cast<int64_t>(rec.x) + row0 + row) * R + 4 * c) = make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
+    }
+}
+
+// ---- host side ----
+
+constexpr int kWorkgroups = 256;  // one on a compute unit
+
+// Rows of a tile.
+static int tile_rows(int B, int64_t T, int64_t max_kv_len, int H) {
+    (void)max_kv_len;
+    return T * H <= 32ll * B ? 32 : 64;
+}
+
+size_t latent_workspace_bytes_bf16(int B, int64_t T, int64_t max_kv_len, int H, int R) {
+    (void)B, (void)T, (void)max_kv_len, (void)H;
+    return latent_parts_layout(kWorkgroups, 64, R).total;
+}
+
+template <int R, int M, bool KV8>
+static int launch_latent(const void* q, const LatentBatch& b, int H, float scale, void* out, void* workspace, hipStream_t stream) {
+    const LatentSplit split = {H, 1, M, kWorkgroups};
+    const LatentParts parts = latent_parts(workspace, latent_parts_layout(kWorkgroups, M, R));
+    constexpr int lds = LatentShape<R, M, KV8>::kBytes;
+    {
+        ProfScope scope(kProfLatent, stream);
+        hipLaunchKernelGGL((latent_bf16_kernel<R, M, KV8>), dim3(kWorkgroups), dim3(256), lds, stream, static_cast<const __hip_bfloat16*>(q), b, split,
+                           scale * 1.4426950408889634f, static_cast<__hip_bfloat16*>(out), parts);
+    }
+    PA_HIP(hipGetLastError());
+    {
+        ProfScope scope(kProfLatentMerge, stream);
+        hipLaunchKernelGGL((latent_merge_kernel<R>), dim3(kWorkgroups, M / kJoinRows), dim3(256), 0, stream, parts, M, static_cast<__hip_bfloat16*>(out));
+    }
+    PA_HIP(hipGetLastError());
+    return PA_OK;
+}
+
+int latent_attention_bf16(const void* q, const LatentBatch& b, int64_t max_kv_len, int H, int R, bool kv8, float scale, void* out, void* workspace,
+                          hipStream_t stream) {
+    const int M = tile_rows(b.B, b.T, max_kv_len, H);
+    if (!kv8) {
+        if (R == 512) return M == 32 ? launch_latent<512, 32, false>(q, b, H, scale, out, workspace, stream) : launch_latent<512, 64, false>(q, b, H, scale, out, workspace, stream);
+        return M == 32 ? launch_latent<256, 32, false>(q, b, H, scale, out, workspace, stream) : launch_latent<256, 64, false>(q, b, H, scale, out, workspace, stream);
+    }
+    if (R == 512) return M == 32 ? launch_latent<512, 32, true>(q, b, H, scale, out, workspace, stream) : launch_latent<512, 64, true>(q, b, H, scale, out, workspace, stream);
+    return M == 32 ? launch_latent<256, 32, true>(q, b, H, scale, out, workspace, stream) : launch_latent<256, 64, true>(q, b, H, scale, out, workspace, stream);
+}
+
+}  // namespace pa
