@@ -11,6 +11,9 @@ size_t latent_expanded_rows_bytes(int64_t T, int H, int R);
 size_t latent_workspace_bytes_bf16(int B, int64_t T, int64_t max_kv_len, int H, int R);
 int latent_attention_bf16(const void* q, const LatentBatch& b, int64_t max_kv_len, int H, int R, bool kv8, float scale, void* out, void* workspace,
                           hipStream_t stream);
+size_t latent_expanded_bytes(int B, int64_t T, int64_t max_kv_len, int H, int R, int N, int64_t num_slots);
+int latent_expanded_bf16(const void* q, const LatentBatch& b, const void* w_k, const void* w_v, int64_t max_kv_len, int H, int R, int N, bool kv8,
+                         float scale, void* out, void* workspace, hipStream_t stream);
 
 constexpr int kMaxRequests = 65536;
 
@@ -66,8 +69,8 @@ extern "C" int pa_latent_attention(const void* q_ext, const void* c_ext, const v
 
 extern "C" size_t pa_latent_expanded_workspace_bytes(int B, int64_t T, int64_t max_kv_len, int H, int R, int P, int N, int64_t num_slots, int dtype) {
     if (!pa::sizes_ok(B, T, max_kv_len, H, R, P, dtype) || (N != 64 && N != 128) || num_slots <= 0 || num_slots > INT32_MAX) return 0;
-    const size_t n = pa::latent_expanded_rows_bytes(T, H, R);
-    return n < 256 ? 256 : n;
+    const size_t n = dtype == PA_F32 ? pa::latent_expanded_rows_bytes(T, H, R) : pa::latent_expanded_bytes(B, T, max_kv_len, H, R, N, num_slots);
+    return n == 0 || n >= 256 ? n : 256;
 }
 
 extern "C" int pa_latent_attention_expanded(const void* q_ext, const void* c_ext, const void* w_k, const void* w_v, const void* latent_pool,
@@ -82,8 +85,11 @@ extern "C" int pa_latent_attention_expanded(const void* q_ext, const void* c_ext
     const size_t need = pa_latent_expanded_workspace_bytes(B, T, max_kv_len, H, R, P, N, num_slots, dtype);
     if (const int rc = pa::check(fn, q_ext, b, max_kv_len, H, R, P, dtype, scale, out, workspace, workspace_bytes, need, &nothing)) return rc;
     if (nothing) return PA_OK;
+    PA_REQUIRE(need != 0, "%s: batch too large", fn);
     PA_REQUIRE(w_k && w_v, "%s: NULL pointer", fn);
     PA_REQUIRE(pa::aligned16(w_k) && pa::aligned16(w_v), "%s: tensors must be 16-byte aligned", fn);
     PA_REQUIRE(out != w_k && out != w_v, "%s: out aliases an input", fn);
+    if (dtype != PA_F32)
+        return pa::latent_expanded_bf16(q_ext, b, w_k, w_v, max_kv_len, H, R, N, dtype == PA_BF16_KV8, scale, out, workspace, static_cast<hipStream_t>(stream));
     return pa::latent_expanded_rows(q_ext, b, w_k, w_v, H, R, N, dtype, scale, out, workspace, static_cast<hipStream_t>(stream));
 }

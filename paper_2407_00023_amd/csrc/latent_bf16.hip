@@ -29,6 +29,7 @@
 #include <type_traits>
 
 #include "fp8_rows.h"
+#include "latent_merge.h"
 #include "latent_work.h"
 #include "wave_ops.h"
 
@@ -37,6 +38,7 @@ namespace pa {
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
+constexpr int kStep = 32;       // keys of a step
 constexpr float kGrow = 40.f;  // log2 units
 
 __device__ const uint4 g_zero_row[128] = {};  // stands for keys behind the last one of a tile
@@ -440,7 +442,7 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
             const int part = 2 * wl + (head ? 1 : 0);
             if (!whole) {
                 used[head ? 1 : 0] = true;
-                if (tid == 0) parts.rec[part] = make_int4(static_cast<int>(out_row0), rows_here, (head ? kPartHead : 0) | (last ? kPartLast : 0), 0);
+                if (tid == 0) parts.rec[part] = make_int4(static_cast<int>(out_row0), rows_here, (head ? kPartHead : 0) | (last ? kPartLast : 0), 1);
                 if (tid < rows_here) parts.ml[static_cast<size_t>(part) * M + tid] = make_float2(s_max[tid], row_total(tid));
             }
 #pragma unroll
@@ -481,72 +483,6 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
     if (tid < 2 && !used[tid]) parts.rec[2 * wl + tid] = make_int4(0, 0, 0, 0);
 }
 
-// The parts of a tile joined: workgroup (w, y) of the launch takes the tile that workgroup w of the attention began and did not finish, if there
-// is one, and kJoinRows of its rows.
-constexpr int kJoinRows = 4;
-template <int R>
-__global__ __launch_bounds__(256) void latent_merge_kernel(LatentParts parts, int M, __hip_bfloat16* __restrict__ out) {
-    constexpr int kCols = R / 4, kRowsAtOnce = 256 / kCols;  // threads of a row
-    __shared__ float s_w[512][kJoinRows];
-    const int w = blockIdx.x, n = parts.hdr[6];
-    if (w >= n) return;
-    const int4 rec = parts.rec[2 * w + 1];
-    const int row0 = blockIdx.y * kJoinRows;
-    if (!(rec.z & kPartHead) || row0 >= rec.y) return;
-    // parts: slot 2 w + 1, then 2 (w + 1), 2 (w + 2), ... up to the one that ends the tile
-    const int tid = threadIdx.x, lane = tid & 63;
-    int count = 1;
-    for (bool more = true; more;) {
-        const int i = w + count + lane;
-        const int flags = i < n ? parts.rec[2 * i].z : kPartLast;
-        const unsigned long long ends = __ballot(flags & kPartLast);
-        count += ends ? __builtin_ctzll(ends) + 1 : 64;
-        more = ends == 0;
-    }
-    auto slot = [&](int p) { return p == 0 ? 2 * w + 1 : 2 * (w + p); };
-    const int rows = min(kJoinRows, rec.y - row0);
-    // weights of the parts: 2^(their maximum - the largest) over the sum
-    if (tid < 64 * kJoinRows) {
-        const int row = tid >> 6;
-        if (row < rows) {
-            float mx = -INFINITY, sum = 0.f;
-            for (int p = lane; p < count; p += 64) {
-                const float2 ml = parts.ml[static_cast<size_t>(slot(p)) * M + row0 + row];
-                if (ml.y != 0.f) mx = fmaxf(mx, ml.x);  // (a part whose keys the row does not see says nothing)
-            }
-#pragma unroll
-            for (int off = 1; off < 64; off <<= 1) mx = fmaxf(mx, __shfl_xor(mx, off));
-            const float ref = mx == -INFINITY ? 0.f : mx;
-            for (int p = lane; p < count; p += 64) {
-                const float2 ml = parts.ml[static_cast<size_t>(slot(p)) * M + row0 + row];
-                const float a = ml.y != 0.f ? __builtin_amdgcn_exp2f(ml.x - ref) : 0.f;
-                s_w[p][row] = a;
-                sum += a * ml.y;
-            }
-#pragma unroll
-            for (int off = 1; off < 64; off <<= 1) sum += __shfl_xor(sum, off);
-            for (int p = lane; p < count; p += 64) s_w[p][row] /= sum;
-        }
-    }
-    __syncthreads();
-    const int c = tid % kCols;
-    for (int row = tid / kCols; row < rows; row += kRowsAtOnce) {
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int p = 0; p < count; ++p) {
-            const float a = s_w[p][row];
-            const float4 v = *reinterpret_cast<const float4*>(parts.o + (static_cast<size_t>(slot(p)) * M + row0 + row) * R + 4 * c);
-            if (a != 0.f) {
-                acc.x += a * v.x;
-                acc.y += a * v.y;
-                acc.z += a * v.z;
-                acc.w += a * v.w;
-            }
-        }
-        *reinterpret_cast<uint2*>(out + (static_cast<int64_t>(rec.x) + row0 + row) * R + 4 * c) = make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
-    }
-}
-
 // ---- host side ----
 
 constexpr int kWorkgroups = 256;  // one on a compute unit
@@ -564,7 +500,7 @@ size_t latent_workspace_bytes_bf16(int B, int64_t T, int64_t max_kv_len, int H, 
 
 template <int R, int M, bool KV8>
 static int launch_latent(const void* q, const LatentBatch& b, int H, float scale, void* out, void* workspace, hipStream_t stream) {
-    const LatentSplit split = {H, 1, M, kWorkgroups};
+    const LatentSplit split = {H, 1, M, kStep, INT32_MAX, kWorkgroups};
     const LatentParts parts = latent_parts(workspace, latent_parts_layout(kWorkgroups, M, R));
     constexpr int lds = LatentShape<R, M, KV8>::kBytes;
     {
@@ -575,7 +511,7 @@ static int launch_latent(const void* q, const LatentBatch& b, int H, float scale
     PA_HIP(hipGetLastError());
     {
         ProfScope scope(kProfLatentMerge, stream);
-        hipLaunchKernelGGL((latent_merge_kernel<R>), dim3(kWorkgroups, M / kJoinRows), dim3(256), 0, stream, parts, M, static_cast<__hip_bfloat16*>(out));
+        launch_latent_merge(parts, kWorkgroups, M, R, out, stream);
     }
     PA_HIP(hipGetLastError());
     return PA_OK;

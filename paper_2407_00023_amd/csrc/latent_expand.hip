@@ -1,0 +1,733 @@
+// Latent attention, expanded form, bf16 tensors: keys and values of every head from the latent rows, once per distinct row, then attention over them.
+//
+// A row of q meets N + kRope values of a key and N of a value in place of R + kRope and R, 3.4 times less arithmetic at R = 512, N = 128; the expansion
+// costs 4 N R operations per row and head, as much as 171 rows of q save.  So it is done once for each row the batch sees, however many
+// requests share it:
+//   mark     every slot of the lists takes a number, the first time it is met (a word per slot of the pool, cleared before)
+//   collect  the rows with numbers, decoded, and the extend rows before them, behind one another: A [rows, R + kRope]; the lists become row numbers
+//   expand   K [head, row, N] = A W_k^T, V likewise, on the matrix cores; fp16 out of fp32 sums
+//   attend   softmax(Q K^T + Q_r A_r^T) V
+// Expanded keys and values lie in the workspace for as many heads at a time as fit kExpandedBytes.
+//
+// fp16 and not bf16, because a rounding of keys, one of values and one of probabilities would each cost as much as the result's own: with 11
+// bits they are an eighth of it each.  What fp16 lacks in range is made up for: a block of 64 rows of K or V of a head whose largest value is out of
+// [2^-6, 2^15) is stored times a power of two, and the attention of that head puts it back (the branch `scaled`, which ordinary values never
+// reach); a row of q is brought to a common size by a power of two, which goes into the factor of its scores.
+#include <hip/hip_bf16.h>
+#include <hip/hip_fp16.h>
+
+#include <type_traits>
+
+#include "fp8_rows.h"
+#include "latent_merge.h"
+#include "latent_work.h"
+#include "wave_ops.h"
+
+namespace pa {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr size_t kExpandedBytes = size_t{1} << 30;
+constexpr int kExpWorkgroups = 256;  // one on a compute unit, in both kernels
+constexpr int kExpM = 128;           // rows of q of a tile
+constexpr int kExpStep = 64;         // keys of a step
+constexpr int kBlockRows = 64;       // rows of K or V with one power of two
+
+__device__ const uint4 g_zero_piece[64] = {};
+
+__device__ __forceinline__ unsigned pack_f16x2(float a, float b) {
+    return __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2_t{a, b}), f16x2));
+}
+__device__ __forceinline__ float power_of_two(int k) { return __int_as_float((k + 127) << 23); }  // k in [-126, 127]
+
+struct ExpandArgs {
+    int32_t *hdr;      // [3], [6]: see LatentParts; [8]: distinct cached rows
+    int32_t *scaled;   // [H] some block of this head is stored times a power of two
+    int32_t *v_top;    // [H] largest power of two of a block of V
+    int32_t *map;      // [num_slots]
+    int32_t *list;     // [cached_cap]
+    int32_t *row_of;   // [B][max_keys]
+    __hip_bfloat16* a; // [rows_cap][R + kRope]
+    signed char *k_exp, *v_exp;  // [heads at once][rows_cap / 64]
+    unsigned short *k, *v;       // [heads at once][rows_cap][N] fp16
+    int64_t cached_cap, rows_cap;
+    int max_keys;
+};
+
+__global__ __launch_bounds__(256) void latent_clear_kernel(ExpandArgs x, int64_t num_slots, int H) {
+    const int64_t i0 = blockIdx.x * 256ll + threadIdx.x;
+    for (int64_t i = i0; i < num_slots; i += gridDim.x * 256ll) x.map[i] = -1;
+    for (int64_t i = i0; i < H; i += gridDim.x * 256ll) {
+        x.scaled[i] = 0;
+        x.v_top[i] = 0;
+    }
+    if (i0 == 0) x.hdr[8] = 0;
+}
+
+// A lane per key of a list.  Which number a slot gets depends on the order of atomics; a row's keys, values and results do not.
+__global__ __launch_bounds__(256) void latent_mark_kernel(LatentBatch b, ExpandArgs x, int chunks) {
+    const int r = blockIdx.x / chunks, j = (blockIdx.x - r * chunks) * 256 + threadIdx.x;
+    const int P = min(b.prefix_len[r], x.max_keys);
+    bool first = false;
+    int slot = 0;
+    if (j < P && b.ext_len[r] > 0) {
+        slot = static_cast<int>(min(static_cast<int64_t>(max(b.slot_idx[b.slot_offsets[r] + j], 0)), b.num_slots - 1));  // never outside the pool
+        first = x.map[slot] == -1 && atomicCAS(&x.map[slot], -1, -2) == -1;
+    }
+    const unsigned long long all = __ballot(first);
+    if (all == 0) return;
+    const int lane = threadIdx.x & 63, leader = __builtin_ctzll(all);
+    int at = 0;
+    if (lane == leader) at = atomicAdd(&x.hdr[8], __popcll(all));
+    at = __shfl(at, leader) + __popcll(all & ((1ull << lane) - 1));
+    if (first && at < x.cached_cap) {
+        x.list[at] = slot;
+        x.map[slot] = static_cast<int>(b.T) + at;
+    }
+}
+
+// Waves take rows of A and, when these are done, 64 list entries at a time.
+template <int R, bool KV8>
+__global__ __launch_bounds__(256) void latent_collect_kernel(LatentBatch b, ExpandArgs x) {
+    constexpr int L = R + kRope, PROW = KV8 ? R + 2 * kRope : 2 * L, LPR = R / 8;  // 16-byte pieces of the latent part of a row of A
+    const int lane = threadIdx.x & 63, waves = gridDim.x * 4, wave = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t rows = b.T + min(static_cast<int64_t>(x.hdr[8]), x.cached_cap);
+    const unsigned char* const pool = static_cast<const unsigned char*>(b.pool);
+    for (int64_t row = wave; row < rows; row += waves) {
+        uint4* const to = reinterpret_cast<uint4*>(x.a + row * L);
+        if (row < b.T || !KV8) {
+            const uint4* const from = row < b.T ? reinterpret_cast<const uint4*>(static_cast<const __hip_bfloat16*>(b.c_ext) + row * L)
+                                                : reinterpret_cast<const uint4*>(pool + static_cast<int64_t>(x.list[row - b.T]) * PROW);
+            for (int c = lane; c < L / 8; c += 64) to[c] = from[c];
+        } else if constexpr (KV8) {
+            const int64_t slot = x.list[row - b.T];
+            const unsigned char* const from = pool + slot * PROW;
+            const float two_k = fp8_scale(reinterpret_cast<const signed char*>(pool + b.num_slots * PROW)[slot]);
+            if (lane < LPR) {
+                const uint2 codes = reinterpret_cast<const uint2*>(from)[lane];
+                const uint2 p = fp8_decode4(codes.x, two_k), q = fp8_decode4(codes.y, two_k);
+                to[lane] = make_uint4(p.x, p.y, q.x, q.y);
+            }
+            if (lane < kRope / 8) to[LPR + lane] = reinterpret_cast<const uint4*>(from + R)[lane];
+        }
+    }
+    const int chunks = (x.max_keys + 63) / 64;
+    for (int64_t i = wave; i < static_cast<int64_t>(b.B) * chunks; i += waves) {
+        const int r = static_cast<int>(i / chunks), j = static_cast<int>(i - static_cast<int64_t>(r) * chunks) * 64 + lane;
+        if (j < min(b.prefix_len[r], x.max_keys) && b.ext_len[r] > 0) {
+            const int64_t slot = min(static_cast<int64_t>(max(b.slot_idx[b.slot_offsets[r] + j], 0)), b.num_slots - 1);
+            x.row_of[static_cast<int64_t>(r) * x.max_keys + j] = x.map[slot];
+        }
+    }
+}
+
+// K and V of the heads h0 .. h0 + heads - 1.  The unit of work is 256 rows by 128 of a head's 2 N columns (its keys, then its values), the units of one set
+// of columns behind one another; a workgroup takes an equal share of them.  The 128 columns of W stay in LDS, 128 KB at R = 512; a wave
+// multiplies 64 rows, straight from memory, so that a fragment of W is read from LDS for four products and nothing is waited for but the first load of W.
+template <int R, int N>
+__global__ __launch_bounds__(256, 1) void latent_expand_kernel(ExpandArgs x, const __hip_bfloat16* __restrict__ w_k, const __hip_bfloat16* __restrict__ w_v,
+                                                               int64_t T, int h0, int heads) {
+    constexpr int L = R + kRope, KS = R / 32, kSets = 2 * N / 128;  // sets of 128 columns per head
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    auto* const lds = (__attribute__((address_space(3))) unsigned char*)smem;
+    const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem));
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g4 = lane >> 4;
+    const int64_t rows = T + min(static_cast<int64_t>(x.hdr[8]), x.cached_cap);
+    const int64_t blocks = (rows + 255) / 256, units = blocks * heads * kSets;
+    const int wg = blockIdx.x;
+    int64_t unit = units * wg / gridDim.x;
+    const int64_t end = units * (wg + 1) / gridDim.x;
+    int have = -1;
+    for (; unit < end; ++unit) {
+        const int set = static_cast<int>(unit / blocks), h = set / kSets;
+        const int64_t row0 = (unit - set * blocks) * 256 + 64 * wave;
+        if (set != have) {
+            have = set;
+            lds_barrier();  // (nobody reads the old columns any more)
+            constexpr int kRowsPerLoad = 512 / R;
+            for (int i = wave; i < 128 / kRowsPerLoad; i += 4) {
+                const int row = i * kRowsPerLoad + lane / (64 / kRowsPerLoad);
+                const int col = (set % kSets) * 128 + row;  // among the head's 2 N
+                const __hip_bfloat16* const from = (col < N ? w_k : w_v) + (static_cast<int64_t>(h0 + h) * N + (col < N ? col : col - N)) * R;
+                load_to_lds_16(from + 8 * ((lane & (64 / kRowsPerLoad - 1)) ^ (row & 15)), lds0 + i * 1024);
+            }
+            wait_vm_all();
+            lds_barrier();
+        }
+        f32x4 acc[8][4];
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[c][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const uint4* from[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) from[r] = reinterpret_cast<const uint4*>(x.a + min(row0 + 16 * r + n, rows - 1) * L) + g4;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            bf16x8 af[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) af[r] = __builtin_bit_cast(bf16x8, from[r][4 * s]);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                const bf16x8 wf = *reinterpret_cast<__attribute__((address_space(3))) const bf16x8*>(lds + (16 * c + n) * 2 * R + 16 * ((4 * s + g4) ^ n));
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, af[r], acc[c][r], 0, 0, 0);
+            }
+        }
+        // lane: row 16 r + n, columns 16 c + 4 g4 .. + 3
+        constexpr int CK = N / 16;  // column blocks of one of the head's two matrices
+#pragma unroll
+        for (int part = 0; part < 8 / CK; ++part) {
+            const bool is_v = (set % kSets) * 128 + part * N >= N;
+            float top = 0.f;
+#pragma unroll
+            for (int c = part * CK; c < (part + 1) * CK; ++c)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float y = fabsf(acc[c][r][i]);
+                        if (row0 + 16 * r + n < rows && y < INFINITY) top = fmaxf(top, y);
+                    }
+#pragma unroll
+            for (int off = 1; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
+            int e = 0;
+            if (top != 0.f && !(top >= 0.015625f && top < 32768.f)) e = max(min(static_cast<int>(__float_as_uint(top) >> 23) - 127 - 13, 126), -126);
+            const float by = power_of_two(-e);
+            if (row0 < rows && lane == 0) {
+                (is_v ? x.v_exp : x.k_exp)[h * (x.rows_cap / kBlockRows) + row0 / kBlockRows] = static_cast<signed char>(e);
+                if (e != 0) atomicOr(&x.scaled[h0 + h], 1);
+                if (is_v && e > 0) atomicMax(&x.v_top[h0 + h], e);
+            }
+            unsigned short* const to = (is_v ? x.v : x.k) + (h * x.rows_cap + row0) * N;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (row0 + 16 * r + n < rows)
+#pragma unroll
+                    for (int c = part * CK; c < (part + 1) * CK; ++c)
+                        *reinterpret_cast<uint2*>(to + (16 * r + n) * N + (c - part * CK) * 16 + 4 * g4) =
+                            make_uint2(pack_f16x2(acc[c][r][0] * by, acc[c][r][1] * by), pack_f16x2(acc[c][r][2] * by, acc[c][r][3] * by));
+        }
+    }
+}
+
+// XOR of the 16-byte piece of a row in LDS: K is read 16 bytes per lane down 16 rows, V 8 bytes per lane across 32 bytes of 8 rows (by half a wave)
+template <int N>
+__device__ __forceinline__ int swz_k(int row) { return N == 128 ? row & 15 : (row >> 1) & 7; }
+template <int N>
+__device__ __forceinline__ int swz_v(int row) {
+    return N == 128 ? ((row & 3) << 2) | (((row >> 2) & 1) << 1) | ((row >> 3) & 1) : (((row >> 1) & 3) << 1) | ((row >> 3) & 1);
+}
+
+// Attention of the heads h0 .. h0 + heads - 1.  A tile is 128 new tokens of a request and one head.  Four waves, a wave per SIMD: wave w has rows
+// 64 (w & 1) .. + 63 and, of every step of 64 keys, keys 32 (w >> 1) .. + 31, with running maxima and sums of its own, so that a fragment of K or V read from LDS meets
+// four blocks of rows and the waves exchange nothing before the end.  (Own 32 rows and all keys would read twice as much LDS, all it can deliver.)
+// Scores are computed transposed, as S^T = K Q^T: what a lane has of them is what it needs of P^T as an operand of O^T = V^T P^T, if the keys
+// are taken in the order 4 g .. 4 g + 3, 16 + 4 g .. 16 + 4 g + 3 by the lanes 16 g .. 16 g + 15; V^T comes by the transposing LDS read.
+// Rows of three steps are in LDS or on their way there.
+constexpr float kExpGrow = 14.f;  // log2 units that a score may outgrow its row's running maximum by: 2^14 is a large fp16 still
+constexpr int kExpSlots = 3;
+
+template <int N>
+struct ExpShape {
+    static constexpr int kRow = 2 * N, kK = kExpStep * kRow, kR = kExpStep * 2 * kRope, kSlot = 2 * kK + kR;
+    static constexpr int kRowsAt = kExpSlots * kSlot, kBytesRing = kRowsAt + 4 * 2 * 256;
+    static constexpr int kJoin = 2 * 64 * N * 4 + 4 * 64 * 8;  // what two waves leave for the two others at the end; maxima and sums of all
+    static constexpr int kBytes = kBytesRing > kJoin ? kBytesRing : kJoin;
+};
+
+template <int N>
+__global__ __launch_bounds__(256, 1) void latent_expanded_kernel(const __hip_bfloat16* __restrict__ q_ext, LatentBatch b, LatentSplit split, ExpandArgs x, int L,
+                                                                 int H, int h0, float scale_log2e, __hip_bfloat16* __restrict__ out, LatentParts parts) {
+    using X = ExpShape<N>;
+    constexpr int QW = N + kRope, KS = N / 32, KSR = kRope / 32, RB = 4, NB = N / 16;
+    constexpr int RPL = 1024 / X::kRow;                         // K or V rows of a 1 KB load
+    constexpr int kLoads = 2 * 16 / RPL + 2;                    // loads per wave and step: 16 rows of K and of V, 16 of the rotary parts
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g4 = lane >> 4;
+    int wl = 0, at_work = 0;
+    LatentPlace at, end;
+    bool over = false;
+    const bool any = latent_share(b, split, blockIdx.x, reinterpret_cast<LatentScratch*>(smem), &wl, &at_work, &at, &end, &over);
+    if (blockIdx.x == 0 && tid == 0) {
+        parts.hdr[3] = over;
+        parts.hdr[6] = at_work;
+    }
+    if (!any) return;
+    const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem));
+    auto* const lds = (__attribute__((address_space(3))) unsigned char*)smem;
+    int* const s_rows = reinterpret_cast<int*>(smem + X::kRowsAt) + wave * 128;
+    const int wrow = 64 * (wave & 1), kg = wave >> 1;
+
+    // LDS read addresses within a slot
+    unsigned k_at[KS < 4 ? KS : 4], r_at[KSR];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) k_at[s] = (32 * kg + n) * X::kRow + 16 * ((4 * s + g4) ^ swz_k<N>(n));
+#pragma unroll
+    for (int s = 0; s < KSR; ++s) r_at[s] = 2 * X::kK + (32 * kg + n) * 2 * kRope + 16 * ((4 * s + g4) ^ ((n >> 1) & 7));
+    unsigned v_at;  // and 32 cb more, by XOR; the second half of the keys 16 rows on (whose XOR is the same)
+    {
+        const int row = 4 * g4 + (n >> 2);
+        v_at = X::kK + (32 * kg + row) * X::kRow + 16 * (((n & 3) >> 1) ^ swz_v<N>(row)) + 8 * (n & 1);
+    }
+
+    bool used[2] = {false, false};
+    while (!(at.r == end.r && at.tile == end.tile && at.k == end.k)) {
+        bool unused = false;
+        LatentRequest req = latent_request(b, split, at.r, &unused);
+        req.P = __builtin_amdgcn_readfirstlane(req.P);
+        req.rows = __builtin_amdgcn_readfirstlane(req.rows);
+        req.tiles = __builtin_amdgcn_readfirstlane(req.tiles);
+        if (at.tile >= req.tiles) {
+            if (++at.r >= b.B) break;
+            at.tile = at.k = 0;
+            continue;
+        }
+        const int per = req.tiles / split.copies, copy = at.tile / per, tile = at.tile - copy * per;
+        const int P = req.P, row0 = tile * kExpM, rows_here = min(kExpM, req.rows - row0), h = h0 + copy;
+        const int64_t e0 = __builtin_amdgcn_readfirstlane(b.ext_offsets[at.r]);
+        const int32_t* const row_of = x.row_of + static_cast<int64_t>(at.r) * x.max_keys;
+        const int key_end = P + row0 + rows_here, all_steps = (key_end + kExpStep - 1) / kExpStep;
+        const int k0 = at.k, k1 = at.r == end.r && at.tile == end.tile ? end.k : all_steps, steps = k1 - k0;
+        const bool wave_on = wrow < rows_here;
+        const int vis_min = P + row0 + min(wrow, rows_here - 1) + 1;  // every row of the wave sees the keys before this one
+        const bool scaled = __builtin_amdgcn_readfirstlane(x.scaled[h]) != 0;
+        const int v_top = __builtin_amdgcn_readfirstlane(x.v_top[h]);
+        const unsigned char* const k_rows = reinterpret_cast<const unsigned char*>(x.k + copy * x.rows_cap * N);
+        const unsigned char* const v_rows = reinterpret_cast<const unsigned char*>(x.v + copy * x.rows_cap * N);
+        const unsigned char* const a_rows = reinterpret_cast<const unsigned char*>(x.a) + 2 * (L - kRope);
+        const signed char* const k_exp = x.k_exp + copy * (x.rows_cap / kBlockRows);
+        const signed char* const v_exp = x.v_exp + copy * (x.rows_cap / kBlockRows);
+
+        // ---- loads of a step: the wave's rows 16 wave .. + 15 ----
+        // row numbers of four steps from step k0 + 4 blk on, lane: step lane / 16, row lane % 16
+        auto load_row_numbers = [&](int blk) {
+            const int first = (k0 + 4 * blk) * kExpStep;
+            if (first < P) {
+                const int j = first + (lane >> 4) * kExpStep + 16 * wave + (lane & 15);
+                load_to_lds_4(row_of + min(j, P - 1), lds0 + X::kRowsAt + wave * 512 + (blk & 1) * 256);
+            }
+        };
+        auto issue = [&](int rel) {
+            const int j0 = (k0 + rel) * kExpStep + 16 * wave;
+            const int* const rn = s_rows + ((rel >> 2) & 1) * 64 + (rel & 3) * 16;
+            const unsigned slot = lds0 + (rel % kExpSlots) * X::kSlot;
+            auto number = [&](int row) -> int64_t { return j0 + row < P ? rn[row] : e0 + (j0 + row - P); };
+            auto from = [&](const unsigned char* base, int row, int64_t stride, int piece) {
+                const unsigned char* const p = base + number(row) * stride + 16 * piece;
+                return j0 + row < key_end ? p : reinterpret_cast<const unsigned char*>(g_zero_piece) + 16 * piece;
+            };
+#pragma unroll
+            for (int i = 0; i < 16 / RPL; ++i) {
+                const int row = i * RPL + lane / (64 / RPL), piece = lane & (64 / RPL - 1);
+                load_to_lds_16(from(k_rows, row, X::kRow, piece ^ swz_k<N>(row)), slot + 16 * wave * X::kRow + i * 1024);
+                load_to_lds_16(from(v_rows, row, X::kRow, piece ^ swz_v<N>(row)), slot + X::kK + 16 * wave * X::kRow + i * 1024);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int row = 8 * i + (lane >> 3);
+                load_to_lds_16(from(a_rows, row, 2 * L, (lane & 7) ^ ((row >> 1) & 7)), slot + 2 * X::kK + 16 * wave * 2 * kRope + i * 1024);
+            }
+        };
+
+        // ---- the wave's rows of Q, times a power of two that brings the largest of a row to [2^8, 2^9) ----
+        load_row_numbers(0);
+        f16x8 q[RB][KS];
+        bf16x8 qr[RB][KSR];
+        float c[RB];
+        int vis[RB];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            const int row = min(wrow + 16 * rb + n, rows_here - 1);  // (rows behind the last repeat it)
+            vis[rb] = P + row0 + row + 1;
+            const uint4* const src = reinterpret_cast<const uint4*>(q_ext + ((e0 + row0 + row) * H + h) * QW);
+            uint4 raw[KS + KSR];
+            unsigned top = 0;
+#pragma unroll
+            for (int s = 0; s < KS + KSR; ++s) {
+                raw[s] = src[4 * s + g4];
+                const unsigned w[4] = {raw[s].x, raw[s].y, raw[s].z, raw[s].w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = max(top, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
+            }
+            top = max(top, static_cast<unsigned>(__shfl_xor(static_cast<int>(top), 16)));
+            top = max(top, static_cast<unsigned>(__shfl_xor(static_cast<int>(top), 32)));
+            const int e = static_cast<int>(top >> 7);
+            const int k = e == 0 || e == 255 ? 0 : max(min(e - 127 - 8, 126), -126);
+            const float by = power_of_two(-k);
+            c[rb] = scale_log2e * power_of_two(k);
+#pragma unroll
+            for (int s = 0; s < KS + KSR; ++s) {
+                const unsigned w[4] = {raw[s].x, raw[s].y, raw[s].z, raw[s].w};
+                unsigned y[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float lo = __uint_as_float(w[i] << 16) * by, hi = __uint_as_float(w[i] & 0xFFFF0000u) * by;
+                    y[i] = s < KS ? pack_f16x2(lo, hi) : pack_bf16x2(lo, hi);
+                }
+                const uint4 z = make_uint4(y[0], y[1], y[2], y[3]);
+                if (s < KS) q[rb][s] = __builtin_bit_cast(f16x8, z);
+                else qr[rb][s - KS] = __builtin_bit_cast(bf16x8, z);
+            }
+        }
+        wait_vm_all();
+        load_row_numbers(1);
+        issue(0);
+        if (steps > 1) issue(1);
+
+        // ---- the pieces of a step ----
+        f32x4 sc[2][RB];
+        // the row number of a key, and its power of two
+        auto exponent = [&](const signed char* of, int j) -> int {
+            if (j >= key_end) return 0;
+            return of[(j < P ? row_of[j] : e0 + (j - P)) / kBlockRows];
+        };
+        auto scores = [&](int rel) __attribute__((always_inline)) {
+            const unsigned slot = (rel % kExpSlots) * X::kSlot;
+            const int j0 = (k0 + rel) * kExpStep + 32 * kg;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) sc[kb][rb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    const f16x8 kf = *reinterpret_cast<__attribute__((address_space(3))) const f16x8*>(lds + (k_at[s] + slot) + kb * 16 * X::kRow);
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) sc[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q[rb][s], sc[kb][rb], 0, 0, 0);
+                }
+            if (scaled) {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float by = power_of_two(exponent(k_exp, j0 + 16 * kb + 4 * g4 + i));
+#pragma unroll
+                        for (int rb = 0; rb < RB; ++rb) sc[kb][rb][i] *= by;
+                    }
+            }
+#pragma unroll
+            for (int s = 0; s < KSR; ++s)
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    const bf16x8 kf = *reinterpret_cast<__attribute__((address_space(3))) const bf16x8*>(lds + (r_at[s] + slot) + kb * 16 * 2 * kRope);
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) sc[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qr[rb][s], sc[kb][rb], 0, 0, 0);
+                }
+            if (j0 + 32 > vis_min) {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (j0 + 16 * kb + 4 * g4 + i >= vis[rb]) sc[kb][rb][i] = -INFINITY;
+            }
+        };
+        float m[RB], l[RB];
+        bool fresh = true;  // no maxima yet: the wave has seen no key
+        auto largest = [&](int rb) {
+            float mx = sc[0][rb][0];
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[kb][rb][i]);
+            return mx * c[rb];
+        };
+        bool odd_seen = false;
+        f16x8 pr[RB];
+        auto probabilities = [&](int rel) __attribute__((always_inline)) {
+            float by[2][4];
+            if (scaled) {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) by[kb][i] = power_of_two(max(exponent(v_exp, (k0 + rel) * kExpStep + 32 * kg + 16 * kb + 4 * g4 + i) - v_top, -126));
+            }
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                float p[2][4];
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        p[kb][i] = __builtin_amdgcn_exp2f(fmaf(sc[kb][rb][i], c[rb], -m[rb]));
+                        l[rb] += p[kb][i];
+                        if (scaled) p[kb][i] *= by[kb][i];
+                    }
+                pr[rb] = __builtin_bit_cast(f16x8, make_uint4(pack_f16x2(p[0][0], p[0][1]), pack_f16x2(p[0][2], p[0][3]), pack_f16x2(p[1][0], p[1][1]),
+                                                              pack_f16x2(p[1][2], p[1][3])));
+            }
+        };
+        auto output = [&](int rel, f32x4 (&o)[RB][NB], auto masked) __attribute__((always_inline)) {
+            const unsigned slot = (rel % kExpSlots) * X::kSlot;
+#pragma unroll
+            for (int cb = 0; cb < NB; ++cb) {
+                const unsigned a = (v_at ^ (32 * cb)) + slot;
+                s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + a));
+                s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + a + 16 * X::kRow));
+                s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                if constexpr (decltype(masked)::value) {
+                    // 0 times an infinity or NaN of a key that some row does not see would be NaN: such values are given to the rows that see them
+                    // at the end instead
+                    bool odd = false;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if ((v[e] & 0x7C00) == 0x7C00) {
+                            odd = true;
+                            v[e] = 0;
+                        }
+                    if (__any(odd)) odd_seen = true;
+                }
+                const f16x8 vf = __builtin_bit_cast(f16x8, v);
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) o[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pr[rb], o[rb][cb], 0, 0, 0);
+            }
+        };
+
+        // ---- the loop ----
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) m[rb] = l[rb] = 0.f;
+        bool flushed = false;
+        // scratch memory of the wave, this lane's part: row 16 rb + n, columns 16 cb + 4 g4 .. + 3
+        float* const scratch = parts.o + ((static_cast<size_t>(2 * split.n_wg + 2 * wl) + kg) * kExpM + wrow + n) * N + 4 * g4;
+        if (steps > 1) wait_vm<kLoads>();
+        else wait_vm_all();
+        lds_barrier();
+        int rel = 0;
+        f32x4 o[RB][NB];
+        bool grown = true;
+        while (true) {
+            if (grown) {
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                    for (int cb = 0; cb < NB; ++cb) o[rb][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
+                grown = false;
+            }
+            while (rel < steps) {
+                // (a wave without rows, or whose rows see none of these keys, only loads)
+                const int j0 = (k0 + rel) * kExpStep + 32 * kg;
+                const bool on = wave_on && j0 < vis_min + 63;
+                if (on) {
+                    scores(rel);
+                    bool outgrown = false;
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) outgrown |= largest(rb) - m[rb] > kExpGrow;
+                    if (fresh || __any(outgrown)) {
+                        grown = true;
+                        break;
+                    }
+                }
+                if ((rel & 3) == 2) load_row_numbers((rel + 2) / 4 + 1);
+                if (rel + 2 < steps) issue(rel + 2);
+                if (on) {
+                    probabilities(rel);
+                    if (j0 + 32 <= vis_min) output(rel, o, std::false_type{});
+                    else output(rel, o, std::true_type{});
+                }
+                if (rel + 2 < steps) wait_vm<kLoads>();
+                else wait_vm_all();
+                lds_barrier();
+                ++rel;
+            }
+            if (!grown) break;
+            // new maxima, from the scores at hand; what has been summed up moves to memory, multiplied accordingly
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                const float mx = row_max(largest(rb));
+                const float mn = fresh ? (mx == -INFINITY ? 0.f : mx) : fmaxf(mx, m[rb]);
+                const float a = fresh ? 0.f : __builtin_amdgcn_exp2f(m[rb] - mn);
+                if (!fresh) {
+#pragma unroll
+                    for (int cb = 0; cb < NB; ++cb) {
+                        f32x4* const to = reinterpret_cast<f32x4*>(scratch + 16 * rb * N + 16 * cb);
+                        f32x4 y = o[rb][cb];
+                        if (flushed) y += *to;
+                        *to = y * a;
+                    }
+                }
+                l[rb] *= a;
+                m[rb] = mn;
+            }
+            if (!fresh) flushed = true;
+            fresh = false;
+        }
+
+        // ---- the waves that share rows are joined; the end of the tile, or of the workgroup's part of it ----
+        float2* const s_ml = reinterpret_cast<float2*>(smem + 2 * 64 * N * 4);  // [4][64] maximum and sum
+        f32x4* const s_o = reinterpret_cast<f32x4*>(smem + (wave & 1) * 64 * N * 4);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            l[rb] = row_sum(l[rb]);
+            if (fresh) m[rb] = -INFINITY;
+            if (g4 == 0) s_ml[wave * 64 + 16 * rb + n] = make_float2(m[rb], l[rb]);
+            if (flushed)
+#pragma unroll
+                for (int cb = 0; cb < NB; ++cb) o[rb][cb] += *reinterpret_cast<const f32x4*>(scratch + 16 * rb * N + 16 * cb);
+            if (kg == 1)
+#pragma unroll
+                for (int cb = 0; cb < NB; ++cb) s_o[(16 * rb + n) * (N / 4) + ((4 * cb + g4) ^ n)] = o[rb][cb];
+        }
+        odd_seen = __syncthreads_or(odd_seen);
+        const bool head = k0 == 0, last = k1 == all_steps, whole = head && last;
+        const int part = 2 * wl + (head ? 1 : 0);
+        const int64_t out_row0 = (e0 + row0) * H + h;
+        if (!whole) {
+            used[head ? 1 : 0] = true;
+            if (tid == 0) parts.rec[part] = make_int4(static_cast<int>(out_row0), rows_here, (head ? kPartHead : 0) | (last ? kPartLast : 0), H);
+        }
+        if (kg == 0) {
+            const float back = power_of_two(v_top);
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                const int row = wrow + 16 * rb + n;
+                const float2 other = s_ml[(wave + 2) * 64 + 16 * rb + n];
+                // (a side whose keys the row does not see has the sum 0 and says nothing)
+                const float ma = l[rb] == 0.f ? -INFINITY : m[rb], mb = other.y == 0.f ? -INFINITY : other.x;
+                const float mx = fmaxf(ma, mb), ref = mx == -INFINITY ? 0.f : mx;
+                const float wa = l[rb] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ma - ref), wb = other.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(mb - ref);
+                const float sum = l[rb] * wa + other.y * wb;
+                if (row >= rows_here) continue;
+                if (!whole && g4 == 0) parts.ml[static_cast<size_t>(part) * kExpM + row] = make_float2(ref, sum);
+                const float inv = whole ? 1.f / sum : 1.f;
+                const int sees = P + row0 + row + 1;
+#pragma unroll
+                for (int cb = 0; cb < NB; ++cb) {
+                    f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
+                    if (wa != 0.f) y += o[rb][cb] * wa;
+                    if (wb != 0.f) y += s_o[(16 * rb + n) * (N / 4) + ((4 * cb + g4) ^ n)] * wb;
+                    y *= inv;
+                    if (scaled) y *= back;
+                    const int col = 16 * cb + 4 * g4;
+                    if (odd_seen) {
+                        // (a weight is positive: an infinity stays one, two of opposite sign and NaN give NaN; the keys of the blocks they were taken out of)
+                        for (int j = max((P + row0 + min(wrow, rows_here - 1) + 1) & ~31, k0 * kExpStep); j < min(sees, k1 * kExpStep); ++j) {
+                            const int64_t at_row = j < P ? static_cast<int64_t>(row_of[j]) : e0 + (j - P);
+                            const unsigned short* const v4 = x.v + (copy * x.rows_cap + at_row) * N + col;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if ((v4[i] & 0x7C00) == 0x7C00) y[i] += (v4[i] & 0x3FF) ? NAN : (v4[i] & 0x8000) ? -INFINITY : INFINITY;
+                        }
+                    }
+                    if (whole)
+                        *reinterpret_cast<uint2*>(out + (out_row0 + static_cast<int64_t>(row) * H) * N + col) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
+                    else
+                        *reinterpret_cast<f32x4*>(parts.o + (static_cast<size_t>(part) * kExpM + row) * N + col) = y;
+                }
+            }
+        }
+        lds_barrier();
+        ++at.tile;
+        at.k = 0;
+        if (k1 != all_steps) break;
+    }
+    if (tid < 2 && !used[tid]) parts.rec[2 * wl + tid] = make_int4(0, 0, 0, 0);
+}
+
+// ---- host side ----
+
+struct ExpandLayout {
+    int heads;  // at once
+    int64_t cached_cap, rows_cap;
+    size_t scaled, v_top, map, list, row_of, a, k_exp, v_exp, k, v, parts, total;
+};
+static ExpandLayout expand_layout(int B, int64_t T, int64_t max_kv_len, int H, int R, int N, int64_t num_slots) {
+    ExpandLayout l;
+    const int64_t listed = static_cast<int64_t>(B) * max_kv_len;
+    l.cached_cap = listed < num_slots ? listed : num_slots;
+    l.rows_cap = (T + l.cached_cap + kBlockRows - 1) / kBlockRows * kBlockRows;
+    const size_t head_bytes = static_cast<size_t>(l.rows_cap) * N * 4;
+    const int most = static_cast<int>(kExpandedBytes / head_bytes < 1 ? 1 : kExpandedBytes / head_bytes > static_cast<size_t>(H) ? H : kExpandedBytes / head_bytes);
+    const int groups = (H + most - 1) / most;
+    l.heads = (H + groups - 1) / groups;
+    size_t at = 256;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += (bytes + 255) & ~size_t{255};
+        return here;
+    };
+    l.scaled = take(sizeof(int32_t) * H);
+    l.v_top = take(sizeof(int32_t) * H);
+    l.map = take(sizeof(int32_t) * num_slots);
+    l.list = take(sizeof(int32_t) * (l.cached_cap + 1));
+    l.row_of = take(sizeof(int32_t) * (listed + 1));
+    l.a = take(static_cast<size_t>(l.rows_cap) * (R + kRope) * 2);
+    l.k_exp = take(static_cast<size_t>(l.heads) * (l.rows_cap / kBlockRows));
+    l.v_exp = take(static_cast<size_t>(l.heads) * (l.rows_cap / kBlockRows));
+    l.k = take(static_cast<size_t>(l.heads) * l.rows_cap * N * 2);
+    l.v = take(static_cast<size_t>(l.heads) * l.rows_cap * N * 2);
+    l.parts = take(latent_parts_layout(kExpWorkgroups, kExpM, N).total + static_cast<size_t>(kExpWorkgroups) * kExpM * N * sizeof(float));  // (scratch memory: two tiles each)
+    l.total = at;
+    return l;
+}
+
+// 0: too large for the 32-bit row numbers
+size_t latent_expanded_bytes(int B, int64_t T, int64_t max_kv_len, int H, int R, int N, int64_t num_slots) {
+    const int64_t listed = static_cast<int64_t>(B) * (max_kv_len + 256);
+    if (T + (listed < num_slots ? listed : num_slots) > INT32_MAX - kBlockRows || listed / 64 > INT32_MAX) return 0;
+    return expand_layout(B, T, max_kv_len, H, R, N, num_slots).total;
+}
+
+template <int R, int N>
+static int launch_group(const void* q, const LatentBatch& b, const ExpandArgs& x, const void* w_k, const void* w_v, int H, int h0, int heads, float scale,
+                        void* out, void* parts_at, hipStream_t stream) {
+    {
+        ProfScope scope(kProfLatentExpand, stream);
+        hipLaunchKernelGGL((latent_expand_kernel<R, N>), dim3(kExpWorkgroups), dim3(256), 256 * R, stream, x, static_cast<const __hip_bfloat16*>(w_k),
+                           static_cast<const __hip_bfloat16*>(w_v), b.T, h0, heads);
+    }
+    PA_HIP(hipGetLastError());
+    const LatentSplit split = {1, heads, kExpM, kExpStep, x.max_keys, kExpWorkgroups};
+    LatentParts parts = latent_parts(parts_at, latent_parts_layout(kExpWorkgroups, kExpM, N));
+    parts.hdr = x.hdr;
+    {
+        ProfScope scope(kProfLatentExpanded, stream);
+        hipLaunchKernelGGL((latent_expanded_kernel<N>), dim3(kExpWorkgroups), dim3(256), ExpShape<N>::kBytes, stream, static_cast<const __hip_bfloat16*>(q), b, split, x,
+                           R + kRope, H, h0, scale * 1.4426950408889634f, static_cast<__hip_bfloat16*>(out), parts);
+    }
+    PA_HIP(hipGetLastError());
+    {
+        ProfScope scope(kProfLatentMerge, stream);
+        launch_latent_merge(parts, kExpWorkgroups, kExpM, N, out, stream);
+    }
+    PA_HIP(hipGetLastError());
+    return PA_OK;
+}
+
+int latent_expanded_bf16(const void* q, const LatentBatch& b, const void* w_k, const void* w_v, int64_t max_kv_len, int H, int R, int N, bool kv8, float scale,
+                         void* out, void* workspace, hipStream_t stream) {
+    const ExpandLayout l = expand_layout(b.B, b.T, max_kv_len, H, R, N, b.num_slots);
+    unsigned char* const w = static_cast<unsigned char*>(workspace);
+    auto i32 = [&](size_t at) { return reinterpret_cast<int32_t*>(w + at); };
+    const ExpandArgs x = {i32(0), i32(l.scaled), i32(l.v_top), i32(l.map), i32(l.list), i32(l.row_of), reinterpret_cast<__hip_bfloat16*>(w + l.a),
+                          reinterpret_cast<signed char*>(w + l.k_exp), reinterpret_cast<signed char*>(w + l.v_exp), reinterpret_cast<unsigned short*>(w + l.k),
+                          reinterpret_cast<unsigned short*>(w + l.v), l.cached_cap, l.rows_cap, static_cast<int>(max_kv_len)};
+    {
+        ProfScope scope(kProfLatentExpand, stream);
+        const int64_t words = b.num_slots > H ? b.num_slots : H, clear = (words + 255) / 256;
+        hipLaunchKernelGGL(latent_clear_kernel, dim3(static_cast<unsigned>(clear < 2048 ? clear : 2048)), dim3(256), 0, stream, x, b.num_slots, H);
+        const int chunks = static_cast<int>((max_kv_len + 255) / 256);
+        if (chunks > 0) hipLaunchKernelGGL(latent_mark_kernel, dim3(static_cast<unsigned>(b.B) * chunks), dim3(256), 0, stream, b, x, chunks);
+        const dim3 grid(2048);
+        if (R == 512 && kv8) hipLaunchKernelGGL((latent_collect_kernel<512, true>), grid, dim3(256), 0, stream, b, x);
+        else if (R == 512) hipLaunchKernelGGL((latent_collect_kernel<512, false>), grid, dim3(256), 0, stream, b, x);
+        else if (kv8) hipLaunchKernelGGL((latent_collect_kernel<256, true>), grid, dim3(256), 0, stream, b, x);
+        else hipLaunchKernelGGL((latent_collect_kernel<256, false>), grid, dim3(256), 0, stream, b, x);
+    }
+    PA_HIP(hipGetLastError());
+    for (int h0 = 0; h0 < H; h0 += l.heads) {
+        const int heads = H - h0 < l.heads ? H - h0 : l.heads;
+        int rc = PA_OK;
+        if (R == 512) rc = N == 128 ? launch_group<512, 128>(q, b, x, w_k, w_v, H, h0, heads, scale, out, w + l.parts, stream) : launch_group<512, 64>(q, b, x, w_k, w_v, H, h0, heads, scale, out, w + l.parts, stream);
+        else rc = N == 128 ? launch_group<256, 128>(q, b, x, w_k, w_v, H, h0, heads, scale, out, w + l.parts, stream) : launch_group<256, 64>(q, b, x, w_k, w_v, H, h0, heads, scale, out, w + l.parts, stream);
+        if (rc != PA_OK) return rc;
+    }
+    return PA_OK;
+}
+
+}  // namespace pa

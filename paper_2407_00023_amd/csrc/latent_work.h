@@ -16,7 +16,6 @@
 
 namespace pa {
 
-constexpr int kStep = 32;        // keys of a step of the loop
 constexpr int kTileCost = 96;    // in keys
 constexpr int kSnap = 3;         // steps
 constexpr int kMinShare = 128;   // keys, besides kTileCost, that a workgroup has at least
@@ -30,9 +29,11 @@ struct LatentRequest {
 };
 
 struct LatentSplit {
-    int rpt;     // rows per token of a copy
+    int rpt;       // rows per token of a copy
     int copies;
     int M;
+    int step;      // keys of a step of the loop
+    int max_keys;  // of a request
     int n_wg;
 };
 
@@ -51,7 +52,7 @@ __device__ __forceinline__ LatentRequest latent_request(const LatentBatch& b, co
         const int E = b.ext_len[r], e0 = b.ext_offsets[r];
         q.P = min(max(b.prefix_len[r], 0), INT32_MAX / 2);
         if (E > 0) {
-            if (e0 < 0 || E > b.T - e0) *over = true;
+            if (e0 < 0 || E > b.T - e0 || q.P > s.max_keys - E) *over = true;
             else q.rows = E * s.rpt;
             q.tiles = (q.rows + s.M - 1) / s.M * s.copies;
         }
@@ -70,7 +71,7 @@ __device__ __forceinline__ int latent_keys(const LatentSplit& s, const LatentReq
     const int last = min((t + 1) * s.M, q.rows) - 1;
     return q.P + last / s.rpt + 1;
 }
-__device__ __forceinline__ int latent_steps(const LatentSplit& s, const LatentRequest& q, int t) { return (latent_keys(s, q, t) + kStep - 1) / kStep; }
+__device__ __forceinline__ int latent_steps(const LatentSplit& s, const LatentRequest& q, int t) { return (latent_keys(s, q, t) + s.step - 1) / s.step; }
 
 __device__ __forceinline__ int64_t wave_scan_64(int64_t x) {
     const int lane = threadIdx.x & 63;
@@ -195,10 +196,10 @@ __device__ __forceinline__ bool latent_share(const LatentBatch& b, const LatentS
 }
 
 // Partial results: slot 2 w holds what workgroup w did of a tile that it did not begin, slot 2 w + 1 of one that it began and did not finish.
-// Slots 2 n .. 3 n - 1 are the workgroups' scratch memory.  Records of a slot: {first row of the output, rows, kPartHead | kPartLast, 0}; flags 0: nothing.
+// Slots 2 n .. 3 n - 1 are the workgroups' scratch memory.  Records of a slot: {first row of the output, rows, kPartHead | kPartLast, rows of the output from one to the next}; flags 0: nothing.
 constexpr int kPartHead = 1, kPartLast = 2;
 struct LatentParts {
-    int32_t* hdr;   // 64 words; [3]: the batch did not fit
+    int32_t* hdr;   // 64 words; [3]: the batch did not fit; [6]: workgroups at work
     int4* rec;      // [2 n_wg]
     float2* ml;     // [2 n_wg][M]  row maximum (log2 units) and sum
     float* o;       // [3 n_wg][M][width]

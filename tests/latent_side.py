@@ -93,7 +93,8 @@ class Batch:
         of the products' magnitudes; a probability is off by twice that (its own and the maximum's or the sum's) relatively, and
         by 2^-20 for the exponential (its argument, of magnitude up to 2^7, in fp32, and 2 units of the function).  Sums over K
         keys: K 2^-24 sum p |v|.  Expanded form: keys and values are rounded once more, to 2^-11 of the largest of a block of
-        them at worst 2^-21 below its top (a value): h16 on each |k| inside a score, and on each |v|."""
+        them at worst 2^-21 below its top (a value): h16 on each |k| inside a score, and on each |v|; a probability in fp16 is off by
+        2^-25 where that is more (their largest is 1 at least)."""
         dt, h = self.dtype, HALF[self.dtype]
         rows = self.stored() if stored is None else stored
         outs, bounds, t = [], [], 0
@@ -135,6 +136,8 @@ class Batch:
                 b = a * (2 * dz + 2.0 ** -20 + (n + e + 64) * 2.0 ** -24 + hp) + h * out.abs() + 1e-30
                 if form != "absorbed":
                     b = b + p @ grow_v * (1 + h)
+                    if h16:
+                        b = b + 2.0 ** -25 * (~hidden).double() @ mag_v
                 o_r.append(out)
                 b_r.append(b)
             outs.append(torch.stack(o_r, 1))
