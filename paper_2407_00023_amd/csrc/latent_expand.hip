@@ -31,12 +31,11 @@ typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr size_t kExpandedBytes = size_t{1} << 30;
-constexpr int kExpWorkgroups = 256;  // one on a compute unit, in both kernels
+constexpr int kExpandWorkgroups = 256;  // one on a compute unit
+constexpr int kExpWorkgroups = 512;     // two
 constexpr int kExpM = 128;           // rows of q of a tile
-constexpr int kExpStep = 64;         // keys of a step
+constexpr int kExpStep = 32;         // keys of a step
 constexpr int kBlockRows = 64;       // rows of K or V with one power of two
-
-__device__ const uint4 g_zero_piece[64] = {};
 
 __device__ __forceinline__ unsigned pack_f16x2(float a, float b) {
     return __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2_t{a, b}), f16x2));
@@ -222,30 +221,30 @@ __device__ __forceinline__ int swz_v(int row) {
     return N == 128 ? ((row & 3) << 2) | (((row >> 2) & 1) << 1) | ((row >> 3) & 1) : (((row >> 1) & 3) << 1) | ((row >> 3) & 1);
 }
 
-// Attention of the heads h0 .. h0 + heads - 1.  A tile is 128 new tokens of a request and one head.  Four waves, a wave per SIMD: wave w has rows
-// 64 (w & 1) .. + 63 and, of every step of 64 keys, keys 32 (w >> 1) .. + 31, with running maxima and sums of its own, so that a fragment of K or V read from LDS meets
-// four blocks of rows and the waves exchange nothing before the end.  (Own 32 rows and all keys would read twice as much LDS, all it can deliver.)
+// Attention of the heads h0 .. h0 + heads - 1.  A tile is 128 new tokens of a request and one head; a wave has 32 of them and all keys, with running
+// maxima of its own, and exchanges nothing with the others.  Two workgroups on a compute unit, so that the exponentials of one
+// wave of a SIMD pass beside the matrix instructions of the other.
 // Scores are computed transposed, as S^T = K Q^T: what a lane has of them is what it needs of P^T as an operand of O^T = V^T P^T, if the keys
 // are taken in the order 4 g .. 4 g + 3, 16 + 4 g .. 16 + 4 g + 3 by the lanes 16 g .. 16 g + 15; V^T comes by the transposing LDS read.
-// Rows of three steps are in LDS or on their way there.
-constexpr float kExpGrow = 14.f;  // log2 units that a score may outgrow its row's running maximum by: 2^14 is a large fp16 still
+// Rows of three steps of 32 keys are in LDS or on their way there.  A row's maximum moves when a score outgrows it by kExpGrow: the wave leaves the
+// loop, what it has summed up goes to memory, multiplied accordingly, and the accumulators begin anew (inside the loop the compiler
+// would keep a second copy of them).
+constexpr float kExpGrow = 14.f;  // log2 units: 2^14 is a large fp16 still
 constexpr int kExpSlots = 3;
 
 template <int N>
 struct ExpShape {
     static constexpr int kRow = 2 * N, kK = kExpStep * kRow, kR = kExpStep * 2 * kRope, kSlot = 2 * kK + kR;
-    static constexpr int kRowsAt = kExpSlots * kSlot, kBytesRing = kRowsAt + 4 * 2 * 256;
-    static constexpr int kJoin = 2 * 64 * N * 4 + 4 * 64 * 8;  // what two waves leave for the two others at the end; maxima and sums of all
-    static constexpr int kBytes = kBytesRing > kJoin ? kBytesRing : kJoin;
+    static constexpr int kRowsAt = kExpSlots * kSlot, kBytes = kRowsAt + 4 * 2 * 256;
 };
 
 template <int N>
-__global__ __launch_bounds__(256, 1) void latent_expanded_kernel(const __hip_bfloat16* __restrict__ q_ext, LatentBatch b, LatentSplit split, ExpandArgs x, int L,
+__global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfloat16* __restrict__ q_ext, LatentBatch b, LatentSplit split, ExpandArgs x, int L,
                                                                  int H, int h0, float scale_log2e, __hip_bfloat16* __restrict__ out, LatentParts parts) {
     using X = ExpShape<N>;
-    constexpr int QW = N + kRope, KS = N / 32, KSR = kRope / 32, RB = 4, NB = N / 16;
-    constexpr int RPL = 1024 / X::kRow;                         // K or V rows of a 1 KB load
-    constexpr int kLoads = 2 * 16 / RPL + 2;                    // loads per wave and step: 16 rows of K and of V, 16 of the rotary parts
+    constexpr int QW = N + kRope, KS = N / 32, KSR = kRope / 32, RB = 2, NB = N / 16;
+    constexpr int RPL = 1024 / X::kRow, kRowLoads = 8 / RPL;    // K or V rows of a 1 KB load; loads of a wave's 8 rows
+    constexpr int kLoads = 2 * kRowLoads + 1;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g4 = lane >> 4;
     int wl = 0, at_work = 0;
@@ -259,20 +258,23 @@ __global__ __launch_bounds__(256, 1) void latent_expanded_kernel(const __hip_bfl
     if (!any) return;
     const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem));
     auto* const lds = (__attribute__((address_space(3))) unsigned char*)smem;
-    int* const s_rows = reinterpret_cast<int*>(smem + X::kRowsAt) + wave * 128;
-    const int wrow = 64 * (wave & 1), kg = wave >> 1;
+    const int wrow = 32 * wave;
 
     // LDS read addresses within a slot
-    unsigned k_at[KS < 4 ? KS : 4], r_at[KSR];
+    unsigned k_at[KS], r_at[KSR];
 #pragma unroll
-    for (int s = 0; s < KS; ++s) k_at[s] = (32 * kg + n) * X::kRow + 16 * ((4 * s + g4) ^ swz_k<N>(n));
+    for (int s = 0; s < KS; ++s) k_at[s] = n * X::kRow + 16 * ((4 * s + g4) ^ swz_k<N>(n));
 #pragma unroll
-    for (int s = 0; s < KSR; ++s) r_at[s] = 2 * X::kK + (32 * kg + n) * 2 * kRope + 16 * ((4 * s + g4) ^ ((n >> 1) & 7));
+    for (int s = 0; s < KSR; ++s) r_at[s] = 2 * X::kK + n * 2 * kRope + 16 * ((4 * s + g4) ^ ((n >> 1) & 7));
     unsigned v_at;  // and 32 cb more, by XOR; the second half of the keys 16 rows on (whose XOR is the same)
     {
         const int row = 4 * g4 + (n >> 2);
-        v_at = X::kK + (32 * kg + row) * X::kRow + 16 * (((n & 3) >> 1) ^ swz_v<N>(row)) + 8 * (n & 1);
+        v_at = X::kK + row * X::kRow + 16 * (((n & 3) >> 1) ^ swz_v<N>(row)) + 8 * (n & 1);
     }
+    // the pieces of rows that a lane loads: rows RPL i + lane / (64 / RPL) of the wave's 8, i = 0, 1 (the XOR of i is put to these)
+    const int load_row = lane / (64 / RPL), load_piece = lane & (64 / RPL - 1);
+    const unsigned k_piece = 16 * (load_piece ^ swz_k<N>((8 * wave + load_row) & 15)), v_piece = 16 * (load_piece ^ swz_v<N>((8 * wave + load_row) & 15));
+    const unsigned r_piece = 2 * (L - kRope) + 16 * ((lane & 7) ^ ((((8 * wave + (lane >> 3)) & 15) >> 1) & 7));
 
     bool used[2] = {false, false};
     while (!(at.r == end.r && at.tile == end.tile && at.k == end.k)) {
@@ -288,49 +290,43 @@ __global__ __launch_bounds__(256, 1) void latent_expanded_kernel(const __hip_bfl
         }
         const int per = req.tiles / split.copies, copy = at.tile / per, tile = at.tile - copy * per;
         const int P = req.P, row0 = tile * kExpM, rows_here = min(kExpM, req.rows - row0), h = h0 + copy;
-        const int64_t e0 = __builtin_amdgcn_readfirstlane(b.ext_offsets[at.r]);
+        const int e0 = __builtin_amdgcn_readfirstlane(b.ext_offsets[at.r]);
         const int32_t* const row_of = x.row_of + static_cast<int64_t>(at.r) * x.max_keys;
         const int key_end = P + row0 + rows_here, all_steps = (key_end + kExpStep - 1) / kExpStep;
         const int k0 = at.k, k1 = at.r == end.r && at.tile == end.tile ? end.k : all_steps, steps = k1 - k0;
         const bool wave_on = wrow < rows_here;
-        const int vis_min = P + row0 + min(wrow, rows_here - 1) + 1;  // every row of the wave sees the keys before this one
-        const bool scaled = __builtin_amdgcn_readfirstlane(x.scaled[h]) != 0;
-        const int v_top = __builtin_amdgcn_readfirstlane(x.v_top[h]);
+        const int vis_min = P + row0 + min(wrow, rows_here - 1) + 1;                             // every row of the wave sees the keys before this one,
+        const int vis_max = wave_on ? P + row0 + min(wrow + 32, rows_here) : 0;                  // none any from this one on
+        const bool is_scaled = __builtin_amdgcn_readfirstlane(x.scaled[h]) != 0;
         const unsigned char* const k_rows = reinterpret_cast<const unsigned char*>(x.k + copy * x.rows_cap * N);
         const unsigned char* const v_rows = reinterpret_cast<const unsigned char*>(x.v + copy * x.rows_cap * N);
-        const unsigned char* const a_rows = reinterpret_cast<const unsigned char*>(x.a) + 2 * (L - kRope);
-        const signed char* const k_exp = x.k_exp + copy * (x.rows_cap / kBlockRows);
-        const signed char* const v_exp = x.v_exp + copy * (x.rows_cap / kBlockRows);
 
-        // ---- loads of a step: the wave's rows 16 wave .. + 15 ----
-        // row numbers of four steps from step k0 + 4 blk on, lane: step lane / 16, row lane % 16
+        // ---- loads of a step: the wave's rows 8 wave .. + 7 ----
+        // row numbers of eight steps from step k0 + 8 blk on, lane: step lane / 8, row lane % 8
         auto load_row_numbers = [&](int blk) {
-            const int first = (k0 + 4 * blk) * kExpStep;
+            const int first = (k0 + 8 * blk) * kExpStep;
             if (first < P) {
-                const int j = first + (lane >> 4) * kExpStep + 16 * wave + (lane & 15);
+                const int j = first + (lane >> 3) * kExpStep + 8 * wave + (lane & 7);
                 load_to_lds_4(row_of + min(j, P - 1), lds0 + X::kRowsAt + wave * 512 + (blk & 1) * 256);
             }
         };
-        auto issue = [&](int rel) {
-            const int j0 = (k0 + rel) * kExpStep + 16 * wave;
-            const int* const rn = s_rows + ((rel >> 2) & 1) * 64 + (rel & 3) * 16;
+        // (keys behind the last repeat it; offsets of 32 bits: the host has seen to it that they suffice)
+        auto issue = [&](int rel) __attribute__((always_inline)) {
+            const int j0 = (k0 + rel) * kExpStep + 8 * wave;
+            const unsigned rn = X::kRowsAt + wave * 512 + ((rel >> 3) & 1) * 256 + (rel & 7) * 32;
             const unsigned slot = lds0 + (rel % kExpSlots) * X::kSlot;
-            auto number = [&](int row) -> int64_t { return j0 + row < P ? rn[row] : e0 + (j0 + row - P); };
-            auto from = [&](const unsigned char* base, int row, int64_t stride, int piece) {
-                const unsigned char* const p = base + number(row) * stride + 16 * piece;
-                return j0 + row < key_end ? p : reinterpret_cast<const unsigned char*>(g_zero_piece) + 16 * piece;
+            auto number = [&](int row) __attribute__((always_inline)) {
+                const int j = min(j0 + row, key_end - 1);
+                const unsigned listed = *reinterpret_cast<__attribute__((address_space(3))) const unsigned*>(lds + rn + 4 * row);
+                return j < P ? listed : static_cast<unsigned>(e0 + (j - P));
             };
 #pragma unroll
-            for (int i = 0; i < 16 / RPL; ++i) {
-                const int row = i * RPL + lane / (64 / RPL), piece = lane & (64 / RPL - 1);
-                load_to_lds_16(from(k_rows, row, X::kRow, piece ^ swz_k<N>(row)), slot + 16 * wave * X::kRow + i * 1024);
-                load_to_lds_16(from(v_rows, row, X::kRow, piece ^ swz_v<N>(row)), slot + X::kK + 16 * wave * X::kRow + i * 1024);
+            for (int i = 0; i < kRowLoads; ++i) {
+                const unsigned at_row = number(i * RPL + load_row) * X::kRow;
+                load_to_lds_16(k_rows, at_row + (k_piece ^ (64 * i)), slot + 8 * wave * X::kRow + i * 1024);
+                load_to_lds_16(v_rows, at_row + (v_piece ^ (32 * i)), slot + X::kK + 8 * wave * X::kRow + i * 1024);
             }
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int row = 8 * i + (lane >> 3);
-                load_to_lds_16(from(a_rows, row, 2 * L, (lane & 7) ^ ((row >> 1) & 7)), slot + 2 * X::kK + 16 * wave * 2 * kRope + i * 1024);
-            }
+            load_to_lds_16(x.a, number(lane >> 3) * static_cast<unsigned>(2 * L) + r_piece, slot + 2 * X::kK + 8 * wave * 2 * kRope);
         };
 
         // ---- the wave's rows of Q, times a power of two that brings the largest of a row to [2^8, 2^9) ----
@@ -338,12 +334,10 @@ __global__ __launch_bounds__(256, 1) void latent_expanded_kernel(const __hip_bfl
         f16x8 q[RB][KS];
         bf16x8 qr[RB][KSR];
         float c[RB];
-        int vis[RB];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
             const int row = min(wrow + 16 * rb + n, rows_here - 1);  // (rows behind the last repeat it)
-            vis[rb] = P + row0 + row + 1;
-            const uint4* const src = reinterpret_cast<const uint4*>(q_ext + ((e0 + row0 + row) * H + h) * QW);
+            const uint4* const src = reinterpret_cast<const uint4*>(q_ext + (static_cast<int64_t>(e0 + row0 + row) * H + h) * QW);
             uint4 raw[KS + KSR];
             unsigned top = 0;
 #pragma unroll
@@ -377,238 +371,214 @@ __global__ __launch_bounds__(256, 1) void latent_expanded_kernel(const __hip_bfl
         load_row_numbers(1);
         issue(0);
         if (steps > 1) issue(1);
-
-        // ---- the pieces of a step ----
-        f32x4 sc[2][RB];
-        // the row number of a key, and its power of two
-        auto exponent = [&](const signed char* of, int j) -> int {
-            if (j >= key_end) return 0;
-            return of[(j < P ? row_of[j] : e0 + (j - P)) / kBlockRows];
-        };
-        auto scores = [&](int rel) __attribute__((always_inline)) {
-            const unsigned slot = (rel % kExpSlots) * X::kSlot;
-            const int j0 = (k0 + rel) * kExpStep + 32 * kg;
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb) sc[kb][rb] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int s = 0; s < KS; ++s)
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                    const f16x8 kf = *reinterpret_cast<__attribute__((address_space(3))) const f16x8*>(lds + (k_at[s] + slot) + kb * 16 * X::kRow);
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) sc[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q[rb][s], sc[kb][rb], 0, 0, 0);
-                }
-            if (scaled) {
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float by = power_of_two(exponent(k_exp, j0 + 16 * kb + 4 * g4 + i));
-#pragma unroll
-                        for (int rb = 0; rb < RB; ++rb) sc[kb][rb][i] *= by;
-                    }
-            }
-#pragma unroll
-            for (int s = 0; s < KSR; ++s)
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                    const bf16x8 kf = *reinterpret_cast<__attribute__((address_space(3))) const bf16x8*>(lds + (r_at[s] + slot) + kb * 16 * 2 * kRope);
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) sc[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qr[rb][s], sc[kb][rb], 0, 0, 0);
-                }
-            if (j0 + 32 > vis_min) {
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (j0 + 16 * kb + 4 * g4 + i >= vis[rb]) sc[kb][rb][i] = -INFINITY;
-            }
-        };
-        float m[RB], l[RB];
-        bool fresh = true;  // no maxima yet: the wave has seen no key
-        auto largest = [&](int rb) {
-            float mx = sc[0][rb][0];
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[kb][rb][i]);
-            return mx * c[rb];
-        };
-        bool odd_seen = false;
-        f16x8 pr[RB];
-        auto probabilities = [&](int rel) __attribute__((always_inline)) {
-            float by[2][4];
-            if (scaled) {
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) by[kb][i] = power_of_two(max(exponent(v_exp, (k0 + rel) * kExpStep + 32 * kg + 16 * kb + 4 * g4 + i) - v_top, -126));
-            }
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb) {
-                float p[2][4];
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        p[kb][i] = __builtin_amdgcn_exp2f(fmaf(sc[kb][rb][i], c[rb], -m[rb]));
-                        l[rb] += p[kb][i];
-                        if (scaled) p[kb][i] *= by[kb][i];
-                    }
-                pr[rb] = __builtin_bit_cast(f16x8, make_uint4(pack_f16x2(p[0][0], p[0][1]), pack_f16x2(p[0][2], p[0][3]), pack_f16x2(p[1][0], p[1][1]),
-                                                              pack_f16x2(p[1][2], p[1][3])));
-            }
-        };
-        auto output = [&](int rel, f32x4 (&o)[RB][NB], auto masked) __attribute__((always_inline)) {
-            const unsigned slot = (rel % kExpSlots) * X::kSlot;
-#pragma unroll
-            for (int cb = 0; cb < NB; ++cb) {
-                const unsigned a = (v_at ^ (32 * cb)) + slot;
-                s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + a));
-                s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + a + 16 * X::kRow));
-                s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                if constexpr (decltype(masked)::value) {
-                    // 0 times an infinity or NaN of a key that some row does not see would be NaN: such values are given to the rows that see them
-                    // at the end instead
-                    bool odd = false;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if ((v[e] & 0x7C00) == 0x7C00) {
-                            odd = true;
-                            v[e] = 0;
-                        }
-                    if (__any(odd)) odd_seen = true;
-                }
-                const f16x8 vf = __builtin_bit_cast(f16x8, v);
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb) o[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pr[rb], o[rb][cb], 0, 0, 0);
-            }
-        };
-
-        // ---- the loop ----
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) m[rb] = l[rb] = 0.f;
-        bool flushed = false;
-        // scratch memory of the wave, this lane's part: row 16 rb + n, columns 16 cb + 4 g4 .. + 3
-        float* const scratch = parts.o + ((static_cast<size_t>(2 * split.n_wg + 2 * wl) + kg) * kExpM + wrow + n) * N + 4 * g4;
         if (steps > 1) wait_vm<kLoads>();
         else wait_vm_all();
         lds_barrier();
-        int rel = 0;
-        f32x4 o[RB][NB];
-        bool grown = true;
-        while (true) {
-            if (grown) {
+
+        const bool head = k0 == 0, last = k1 == all_steps, whole = head && last;
+        const int part = 2 * wl + (head ? 1 : 0);
+        const int out_row0 = (e0 + row0) * H + h;
+        // The tile, with keys and values as they are (the usual case) or with powers of two of their own.
+        auto walk = [&](auto scaled_c) __attribute__((always_inline)) {
+            constexpr bool scaled = decltype(scaled_c)::value;
+            f32x4 sc[2][RB];
+            // the power of two of a key's or value's block
+            auto exponent = [&](const signed char* of, int j) -> int {
+                return j >= key_end ? 0 : of[copy * (x.rows_cap / kBlockRows) + (j < P ? row_of[j] : e0 + (j - P)) / kBlockRows];
+            };
+            auto scores = [&](int rel) __attribute__((always_inline)) {
+                const unsigned slot = (rel % kExpSlots) * X::kSlot;
+                const int j0 = (k0 + rel) * kExpStep;
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) sc[kb][rb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb) {
+                        const f16x8 kf = *reinterpret_cast<__attribute__((address_space(3))) const f16x8*>(lds + (k_at[s] + slot) + kb * 16 * X::kRow);
+#pragma unroll
+                        for (int rb = 0; rb < RB; ++rb) sc[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q[rb][s], sc[kb][rb], 0, 0, 0);
+                    }
+                if constexpr (scaled) {
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float by = power_of_two(exponent(x.k_exp, j0 + 16 * kb + 4 * g4 + i));
+#pragma unroll
+                            for (int rb = 0; rb < RB; ++rb) sc[kb][rb][i] *= by;
+                        }
+                }
+#pragma unroll
+                for (int s = 0; s < KSR; ++s)
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb) {
+                        const bf16x8 kf = *reinterpret_cast<__attribute__((address_space(3))) const bf16x8*>(lds + (r_at[s] + slot) + kb * 16 * 2 * kRope);
+#pragma unroll
+                        for (int rb = 0; rb < RB; ++rb) sc[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qr[rb][s], sc[kb][rb], 0, 0, 0);
+                    }
+                if (j0 + kExpStep > vis_min) {
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) {
+                        const int sees = P + row0 + min(wrow + 16 * rb + n, rows_here - 1) + 1 - j0 - 4 * g4;
+#pragma unroll
+                        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if (16 * kb + i >= sees) sc[kb][rb][i] = -INFINITY;
+                    }
+                }
+            };
+            float m[RB], l[RB];
+            bool fresh = true, flushed = false, odd_seen = false;  // fresh: no maxima yet, the wave has seen no key
+            auto largest = [&](int rb) __attribute__((always_inline)) {
+                float mx = sc[0][rb][0];
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[kb][rb][i]);
+                return mx * c[rb];
+            };
+            f16x8 pr[RB];
+            auto probabilities = [&](int rel) __attribute__((always_inline)) {
+                float by[2][4];
+                if constexpr (scaled) {
+                    const int v_top = x.v_top[h];
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) by[kb][i] = power_of_two(max(exponent(x.v_exp, (k0 + rel) * kExpStep + 16 * kb + 4 * g4 + i) - v_top, -126));
+                }
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) {
+                    float p[2][4];
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            p[kb][i] = __builtin_amdgcn_exp2f(fmaf(sc[kb][rb][i], c[rb], -m[rb]));
+                            l[rb] += p[kb][i];
+                            if constexpr (scaled) p[kb][i] *= by[kb][i];
+                        }
+                    pr[rb] = __builtin_bit_cast(f16x8, make_uint4(pack_f16x2(p[0][0], p[0][1]), pack_f16x2(p[0][2], p[0][3]), pack_f16x2(p[1][0], p[1][1]),
+                                                                  pack_f16x2(p[1][2], p[1][3])));
+                }
+            };
+            auto output = [&](int rel, f32x4 (&o)[RB][NB], auto masked) __attribute__((always_inline)) {
+                const unsigned slot = (rel % kExpSlots) * X::kSlot, v_here = worked_out_here(v_at);
+#pragma unroll
+                for (int cb = 0; cb < NB; ++cb) {
+                    const unsigned a = (v_here ^ (32 * cb)) + slot;
+                    s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + a));
+                    s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + a + 16 * X::kRow));
+                    s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                    if constexpr (decltype(masked)::value) {
+                        // 0 times an infinity or NaN of a key that some row does not see would be NaN: such values are given to the rows that see
+                        // them at the end instead
+                        bool odd = false;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if ((v[e] & 0x7C00) == 0x7C00) {
+                                odd = true;
+                                v[e] = 0;
+                            }
+                        if (__any(odd)) odd_seen = true;
+                    }
+                    const f16x8 vf = __builtin_bit_cast(f16x8, v);
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) o[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pr[rb], o[rb][cb], 0, 0, 0);
+                }
+            };
+            // scratch memory of the wave, this lane's part: row 16 rb + n, columns 16 cb + 4 g4 .. + 3
+            auto scratch = [&](unsigned lane_now) {
+                return parts.o + (static_cast<size_t>(2 * split.n_wg + wl) * kExpM + wrow + (lane_now & 15)) * N + 4 * (lane_now >> 4);
+            };
+
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) m[rb] = l[rb] = 0.f;
+            int rel = 0;
+            f32x4 o[RB][NB];
+            while (true) {
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
                     for (int cb = 0; cb < NB; ++cb) o[rb][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
-                grown = false;
-            }
-            while (rel < steps) {
-                // (a wave without rows, or whose rows see none of these keys, only loads)
-                const int j0 = (k0 + rel) * kExpStep + 32 * kg;
-                const bool on = wave_on && j0 < vis_min + 63;
-                if (on) {
-                    scores(rel);
-                    bool outgrown = false;
+                bool grown = false;
+                while (rel < steps) {
+                    const int j0 = (k0 + rel) * kExpStep;
+                    const bool on = j0 < vis_max;  // (a wave whose rows see none of these keys only loads)
+                    if (on) {
+                        scores(rel);
+                        bool outgrown = fresh;
 #pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) outgrown |= largest(rb) - m[rb] > kExpGrow;
-                    if (fresh || __any(outgrown)) {
-                        grown = true;
-                        break;
+                        for (int rb = 0; rb < RB; ++rb) outgrown |= largest(rb) - m[rb] > kExpGrow;
+                        if (__any(outgrown)) {
+                            grown = true;
+                            break;
+                        }
                     }
-                }
-                if ((rel & 3) == 2) load_row_numbers((rel + 2) / 4 + 1);
-                if (rel + 2 < steps) issue(rel + 2);
-                if (on) {
-                    probabilities(rel);
-                    if (j0 + 32 <= vis_min) output(rel, o, std::false_type{});
-                    else output(rel, o, std::true_type{});
-                }
-                if (rel + 2 < steps) wait_vm<kLoads>();
-                else wait_vm_all();
-                lds_barrier();
-                ++rel;
-            }
-            if (!grown) break;
-            // new maxima, from the scores at hand; what has been summed up moves to memory, multiplied accordingly
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb) {
-                const float mx = row_max(largest(rb));
-                const float mn = fresh ? (mx == -INFINITY ? 0.f : mx) : fmaxf(mx, m[rb]);
-                const float a = fresh ? 0.f : __builtin_amdgcn_exp2f(m[rb] - mn);
-                if (!fresh) {
-#pragma unroll
-                    for (int cb = 0; cb < NB; ++cb) {
-                        f32x4* const to = reinterpret_cast<f32x4*>(scratch + 16 * rb * N + 16 * cb);
-                        f32x4 y = o[rb][cb];
-                        if (flushed) y += *to;
-                        *to = y * a;
+                    if ((rel & 7) == 6) load_row_numbers((rel + 2) / 8 + 1);
+                    if (rel + 2 < steps) issue(rel + 2);
+                    if (on) {
+                        probabilities(rel);
+                        if (j0 + kExpStep <= vis_min) output(rel, o, std::false_type{});
+                        else output(rel, o, std::true_type{});
                     }
+                    if (rel + 2 < steps) wait_vm<kLoads>();
+                    else wait_vm_all();
+                    lds_barrier();
+                    ++rel;
                 }
-                l[rb] *= a;
-                m[rb] = mn;
+                if (!grown) break;
+                {
+                    // new maxima, from the scores at hand; what has been summed up moves to memory, multiplied accordingly
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) {
+                        const float mx = row_max(largest(rb));
+                        const float mn = fresh ? (mx == -INFINITY ? 0.f : mx) : fmaxf(mx, m[rb]);  // (a row that sees no key yet sees none at all)
+                        const float a = fresh ? 0.f : __builtin_amdgcn_exp2f(m[rb] - mn);
+                        if (!fresh) {
+                            float* const to = scratch(worked_out_here(lane)) + 16 * rb * N;
+#pragma unroll
+                            for (int cb = 0; cb < NB; ++cb) {
+                                f32x4 y = o[rb][cb];
+                                if (flushed) y += *reinterpret_cast<const f32x4*>(to + 16 * cb);
+                                *reinterpret_cast<f32x4*>(to + 16 * cb) = y * a;
+                            }
+                        }
+                        l[rb] *= a;
+                        m[rb] = mn;
+                    }
+                    if (!fresh) flushed = true;
+                    fresh = false;
+                }
             }
-            if (!fresh) flushed = true;
-            fresh = false;
-        }
 
-        // ---- the waves that share rows are joined; the end of the tile, or of the workgroup's part of it ----
-        float2* const s_ml = reinterpret_cast<float2*>(smem + 2 * 64 * N * 4);  // [4][64] maximum and sum
-        f32x4* const s_o = reinterpret_cast<f32x4*>(smem + (wave & 1) * 64 * N * 4);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-            l[rb] = row_sum(l[rb]);
-            if (fresh) m[rb] = -INFINITY;
-            if (g4 == 0) s_ml[wave * 64 + 16 * rb + n] = make_float2(m[rb], l[rb]);
-            if (flushed)
-#pragma unroll
-                for (int cb = 0; cb < NB; ++cb) o[rb][cb] += *reinterpret_cast<const f32x4*>(scratch + 16 * rb * N + 16 * cb);
-            if (kg == 1)
-#pragma unroll
-                for (int cb = 0; cb < NB; ++cb) s_o[(16 * rb + n) * (N / 4) + ((4 * cb + g4) ^ n)] = o[rb][cb];
-        }
-        odd_seen = __syncthreads_or(odd_seen);
-        const bool head = k0 == 0, last = k1 == all_steps, whole = head && last;
-        const int part = 2 * wl + (head ? 1 : 0);
-        const int64_t out_row0 = (e0 + row0) * H + h;
-        if (!whole) {
-            used[head ? 1 : 0] = true;
-            if (tid == 0) parts.rec[part] = make_int4(static_cast<int>(out_row0), rows_here, (head ? kPartHead : 0) | (last ? kPartLast : 0), H);
-        }
-        if (kg == 0) {
-            const float back = power_of_two(v_top);
+            // ---- the end of the tile, or of the workgroup's part of it ----
+            const unsigned lane_now = worked_out_here(lane);
+            const int n = lane_now & 15, g4 = lane_now >> 4;
+            const float back = scaled ? power_of_two(x.v_top[h]) : 1.f;
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
+                const float sum = row_sum(l[rb]);
                 const int row = wrow + 16 * rb + n;
-                const float2 other = s_ml[(wave + 2) * 64 + 16 * rb + n];
-                // (a side whose keys the row does not see has the sum 0 and says nothing)
-                const float ma = l[rb] == 0.f ? -INFINITY : m[rb], mb = other.y == 0.f ? -INFINITY : other.x;
-                const float mx = fmaxf(ma, mb), ref = mx == -INFINITY ? 0.f : mx;
-                const float wa = l[rb] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ma - ref), wb = other.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(mb - ref);
-                const float sum = l[rb] * wa + other.y * wb;
                 if (row >= rows_here) continue;
-                if (!whole && g4 == 0) parts.ml[static_cast<size_t>(part) * kExpM + row] = make_float2(ref, sum);
+                if (!whole && g4 == 0) parts.ml[static_cast<size_t>(part) * kExpM + row] = make_float2(m[rb], sum);
                 const float inv = whole ? 1.f / sum : 1.f;
-                const int sees = P + row0 + row + 1;
 #pragma unroll
                 for (int cb = 0; cb < NB; ++cb) {
-                    f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
-                    if (wa != 0.f) y += o[rb][cb] * wa;
-                    if (wb != 0.f) y += s_o[(16 * rb + n) * (N / 4) + ((4 * cb + g4) ^ n)] * wb;
+                    f32x4 y = o[rb][cb];
+                    if (flushed) y += *reinterpret_cast<const f32x4*>(scratch(lane_now) + 16 * rb * N + 16 * cb);
                     y *= inv;
-                    if (scaled) y *= back;
+                    if constexpr (scaled) y *= back;
                     const int col = 16 * cb + 4 * g4;
                     if (odd_seen) {
                         // (a weight is positive: an infinity stays one, two of opposite sign and NaN give NaN; the keys of the blocks they were taken out of)
-                        for (int j = max((P + row0 + min(wrow, rows_here - 1) + 1) & ~31, k0 * kExpStep); j < min(sees, k1 * kExpStep); ++j) {
-                            const int64_t at_row = j < P ? static_cast<int64_t>(row_of[j]) : e0 + (j - P);
-                            const unsigned short* const v4 = x.v + (copy * x.rows_cap + at_row) * N + col;
+                        for (int j = max(vis_min & ~(kExpStep - 1), k0 * kExpStep); j < min(P + row0 + row + 1, k1 * kExpStep); ++j) {
+                            const int64_t at_row = j < P ? row_of[j] : e0 + (j - P);
+                            const unsigned short* const v4 = reinterpret_cast<const unsigned short*>(v_rows) + at_row * N + col;
 #pragma unroll
                             for (int i = 0; i < 4; ++i)
                                 if ((v4[i] & 0x7C00) == 0x7C00) y[i] += (v4[i] & 0x3FF) ? NAN : (v4[i] & 0x8000) ? -INFINITY : INFINITY;
@@ -620,8 +590,13 @@ __global__ __launch_bounds__(256, 1) void latent_expanded_kernel(const __hip_bfl
                         *reinterpret_cast<f32x4*>(parts.o + (static_cast<size_t>(part) * kExpM + row) * N + col) = y;
                 }
             }
+        };
+        if (is_scaled) walk(std::true_type{});
+        else walk(std::false_type{});
+        if (!whole) {
+            used[head ? 1 : 0] = true;
+            if (tid == 0) parts.rec[part] = make_int4(out_row0, rows_here, (head ? kPartHead : 0) | (last ? kPartLast : 0), H);
         }
-        lds_barrier();
         ++at.tile;
         at.k = 0;
         if (k1 != all_steps) break;
@@ -661,15 +636,16 @@ static ExpandLayout expand_layout(int B, int64_t T, int64_t max_kv_len, int H, i
     l.v_exp = take(static_cast<size_t>(l.heads) * (l.rows_cap / kBlockRows));
     l.k = take(static_cast<size_t>(l.heads) * l.rows_cap * N * 2);
     l.v = take(static_cast<size_t>(l.heads) * l.rows_cap * N * 2);
-    l.parts = take(latent_parts_layout(kExpWorkgroups, kExpM, N).total + static_cast<size_t>(kExpWorkgroups) * kExpM * N * sizeof(float));  // (scratch memory: two tiles each)
+    l.parts = take(latent_parts_layout(kExpWorkgroups, kExpM, N).total);
     l.total = at;
     return l;
 }
 
-// 0: too large for the 32-bit row numbers
+// 0: too many rows for offsets of 32 bits
 size_t latent_expanded_bytes(int B, int64_t T, int64_t max_kv_len, int H, int R, int N, int64_t num_slots) {
     const int64_t listed = static_cast<int64_t>(B) * (max_kv_len + 256);
-    if (T + (listed < num_slots ? listed : num_slots) > INT32_MAX - kBlockRows || listed / 64 > INT32_MAX) return 0;
+    const int64_t rows = T + (listed < num_slots ? listed : num_slots);
+    if (rows + kBlockRows > UINT32_MAX / (2 * (R + kRope)) || listed / 64 > INT32_MAX) return 0;
     return expand_layout(B, T, max_kv_len, H, R, N, num_slots).total;
 }
 
@@ -678,7 +654,7 @@ static int launch_group(const void* q, const LatentBatch& b, const ExpandArgs& x
                         void* out, void* parts_at, hipStream_t stream) {
     {
         ProfScope scope(kProfLatentExpand, stream);
-        hipLaunchKernelGGL((latent_expand_kernel<R, N>), dim3(kExpWorkgroups), dim3(256), 256 * R, stream, x, static_cast<const __hip_bfloat16*>(w_k),
+        hipLaunchKernelGGL((latent_expand_kernel<R, N>), dim3(kExpandWorkgroups), dim3(256), 256 * R, stream, x, static_cast<const __hip_bfloat16*>(w_k),
                            static_cast<const __hip_bfloat16*>(w_v), b.T, h0, heads);
     }
     PA_HIP(hipGetLastError());

@@ -84,6 +84,11 @@ __device__ __forceinline__ unsigned lds_address(const void* p) {
     return static_cast<unsigned>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const unsigned char*)(p)));
 }
 
+// The same value, of which the compiler knows nothing: what is derived from it is worked out here and not kept in registers from before a loop.
+__device__ __forceinline__ unsigned worked_out_here(unsigned x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
 // s_waitcnt vmcnt(N): all but the newest N of the wave's loads have landed.
 template <int N>
 __device__ __forceinline__ void wait_vm() {
