@@ -29,6 +29,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr size_t kExpandedBytes = size_t{1} << 30;
 constexpr int kExpandWorkgroups = 256;  // one on a compute unit
@@ -48,7 +49,7 @@ struct ExpandArgs {
     int32_t *v_top;    // [H] largest power of two of a block of V
     int32_t *map;      // [num_slots]
     int32_t *list;     // [cached_cap]
-    int32_t *row_of;   // [B][max_keys]
+    int32_t *row_of;   // [B][max_keys] rows of A of a request's keys, cached and new
     __hip_bfloat16* a; // [rows_cap][R + kRope]
     signed char *k_exp, *v_exp;  // [heads at once][rows_cap / 64]
     unsigned short *k, *v;       // [heads at once][rows_cap][N] fp16
@@ -88,7 +89,7 @@ __global__ __launch_bounds__(256) void latent_mark_kernel(LatentBatch b, ExpandA
     }
 }
 
-// Waves take rows of A and, when these are done, 64 list entries at a time.
+// Waves take rows of A and, when these are done, 64 keys of a request at a time.
 template <int R, bool KV8>
 __global__ __launch_bounds__(256) void latent_collect_kernel(LatentBatch b, ExpandArgs x) {
     constexpr int L = R + kRope, PROW = KV8 ? R + 2 * kRope : 2 * L, LPR = R / 8;  // 16-byte pieces of the latent part of a row of A
@@ -116,10 +117,14 @@ __global__ __launch_bounds__(256) void latent_collect_kernel(LatentBatch b, Expa
     const int chunks = (x.max_keys + 63) / 64;
     for (int64_t i = wave; i < static_cast<int64_t>(b.B) * chunks; i += waves) {
         const int r = static_cast<int>(i / chunks), j = static_cast<int>(i - static_cast<int64_t>(r) * chunks) * 64 + lane;
-        if (j < min(b.prefix_len[r], x.max_keys) && b.ext_len[r] > 0) {
+        const int P = min(max(b.prefix_len[r], 0), x.max_keys), E = b.ext_len[r];
+        if (E <= 0 || j >= x.max_keys || j - P >= E) continue;
+        int number = b.ext_offsets[r] + (j - P);
+        if (j < P) {
             const int64_t slot = min(static_cast<int64_t>(max(b.slot_idx[b.slot_offsets[r] + j], 0)), b.num_slots - 1);
-            x.row_of[static_cast<int64_t>(r) * x.max_keys + j] = x.map[slot];
+            number = x.map[slot];
         }
+        x.row_of[static_cast<int64_t>(r) * x.max_keys + j] = number;
     }
 }
 
@@ -226,16 +231,17 @@ __device__ __forceinline__ int swz_v(int row) {
 // wave of a SIMD pass beside the matrix instructions of the other.
 // Scores are computed transposed, as S^T = K Q^T: what a lane has of them is what it needs of P^T as an operand of O^T = V^T P^T, if the keys
 // are taken in the order 4 g .. 4 g + 3, 16 + 4 g .. 16 + 4 g + 3 by the lanes 16 g .. 16 g + 15; V^T comes by the transposing LDS read.
-// Rows of three steps of 32 keys are in LDS or on their way there.  A row's maximum moves when a score outgrows it by kExpGrow: the wave leaves the
-// loop, what it has summed up goes to memory, multiplied accordingly, and the accumulators begin anew (inside the loop the compiler
+// In the loop the scores of step i + 1 and the output of step i are computed, the probabilities of step i in between; keys of step i + 3 and values of
+// step i + 2 are on their way to LDS, each in a ring of three.  A row's maximum moves when a lane's probabilities of a step sum to more than kExpMost: the wave leaves
+// the loop, what it has summed up goes to memory, multiplied accordingly, and the accumulators begin anew (inside the loop the compiler
 // would keep a second copy of them).
-constexpr float kExpGrow = 14.f;  // log2 units: 2^14 is a large fp16 still
+constexpr float kExpMost = 16384.f;  // 2^14 is a large fp16 still
 constexpr int kExpSlots = 3;
 
 template <int N>
 struct ExpShape {
     static constexpr int kRow = 2 * N, kK = kExpStep * kRow, kR = kExpStep * 2 * kRope, kSlot = 2 * kK + kR;
-    static constexpr int kRowsAt = kExpSlots * kSlot, kBytes = kRowsAt + 4 * 2 * 256;
+    static constexpr int kRowsAt = kExpSlots * kSlot, kOddAt = kRowsAt + 4 * 2 * 256, kBytes = kOddAt + 16;
 };
 
 template <int N>
@@ -259,6 +265,7 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
     const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem));
     auto* const lds = (__attribute__((address_space(3))) unsigned char*)smem;
     const int wrow = 32 * wave;
+    int* const s_odd = reinterpret_cast<int*>(smem + X::kOddAt);
 
     // LDS read addresses within a slot
     unsigned k_at[KS], r_at[KSR];
@@ -294,39 +301,55 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
         const int32_t* const row_of = x.row_of + static_cast<int64_t>(at.r) * x.max_keys;
         const int key_end = P + row0 + rows_here, all_steps = (key_end + kExpStep - 1) / kExpStep;
         const int k0 = at.k, k1 = at.r == end.r && at.tile == end.tile ? end.k : all_steps, steps = k1 - k0;
-        const bool wave_on = wrow < rows_here;
-        const int vis_min = P + row0 + min(wrow, rows_here - 1) + 1;                             // every row of the wave sees the keys before this one,
-        const int vis_max = wave_on ? P + row0 + min(wrow + 32, rows_here) : 0;                  // none any from this one on
+        const int vis_min = P + row0 + min(wrow, rows_here - 1) + 1;  // every row of the wave sees the keys before this one
         const bool is_scaled = __builtin_amdgcn_readfirstlane(x.scaled[h]) != 0;
         const unsigned char* const k_rows = reinterpret_cast<const unsigned char*>(x.k + copy * x.rows_cap * N);
         const unsigned char* const v_rows = reinterpret_cast<const unsigned char*>(x.v + copy * x.rows_cap * N);
 
         // ---- loads of a step: the wave's rows 8 wave .. + 7 ----
-        // row numbers of eight steps from step k0 + 8 blk on, lane: step lane / 8, row lane % 8
+        // row numbers of eight steps from step k0 + 8 blk on, lane: step lane / 8, row lane % 8 (keys behind the last repeat it)
         auto load_row_numbers = [&](int blk) {
             const int first = (k0 + 8 * blk) * kExpStep;
-            if (first < P) {
-                const int j = first + (lane >> 3) * kExpStep + 8 * wave + (lane & 7);
-                load_to_lds_4(row_of + min(j, P - 1), lds0 + X::kRowsAt + wave * 512 + (blk & 1) * 256);
-            }
+            if (first < key_end)
+                load_to_lds_4(row_of + min(first + (lane >> 3) * kExpStep + 8 * wave + (lane & 7), key_end - 1), lds0 + X::kRowsAt + wave * 512 + (blk & 1) * 256);
         };
-        // (keys behind the last repeat it; offsets of 32 bits: the host has seen to it that they suffice)
-        auto issue = [&](int rel) __attribute__((always_inline)) {
-            const int j0 = (k0 + rel) * kExpStep + 8 * wave;
-            const unsigned rn = X::kRowsAt + wave * 512 + ((rel >> 3) & 1) * 256 + (rel & 7) * 32;
-            const unsigned slot = lds0 + (rel % kExpSlots) * X::kSlot;
-            auto number = [&](int row) __attribute__((always_inline)) {
-                const int j = min(j0 + row, key_end - 1);
-                const unsigned listed = *reinterpret_cast<__attribute__((address_space(3))) const unsigned*>(lds + rn + 4 * row);
-                return j < P ? listed : static_cast<unsigned>(e0 + (j - P));
-            };
+        // (offsets of 32 bits: the host has seen to it that they suffice)
+        auto number = [&](int rel, int row) __attribute__((always_inline)) {
+            return *reinterpret_cast<__attribute__((address_space(3))) const unsigned*>(lds + X::kRowsAt + wave * 512 + (rel & 15) * 32 + 4 * row);
+        };
+        auto issue_k = [&](int rel, unsigned slot) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < kRowLoads; ++i)
+                load_to_lds_16(k_rows, number(rel, i * RPL + load_row) * X::kRow | (k_piece ^ (64 * i)), lds0 + slot + 8 * wave * X::kRow + i * 1024);
+            load_to_lds_16(x.a, __umul24(number(rel, lane >> 3), 2 * L) + r_piece, lds0 + slot + 2 * X::kK + 8 * wave * 2 * kRope);
+        };
+        auto issue_v = [&](int rel, unsigned slot) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < kRowLoads; ++i)
+                load_to_lds_16(v_rows, number(rel, i * RPL + load_row) * X::kRow | (v_piece ^ (32 * i)), lds0 + slot + X::kK + 8 * wave * X::kRow + i * 1024);
+        };
+
+        // Steps with keys that some row of the tile does not see, or behind the last: 0 times an infinity or NaN of such a key would be NaN.  The wave
+        // that loaded a row of V takes such values out of it, and the end of the tile gives them to the rows that see them.
+        auto clean = [&](int rel, unsigned slot) __attribute__((always_inline)) {
+            if ((k0 + rel + 1) * kExpStep <= P + row0 + 1) return;
+            const unsigned at_v = slot + X::kK + 8 * wave * X::kRow + 16 * lane;
 #pragma unroll
             for (int i = 0; i < kRowLoads; ++i) {
-                const unsigned at_row = number(i * RPL + load_row) * X::kRow;
-                load_to_lds_16(k_rows, at_row + (k_piece ^ (64 * i)), slot + 8 * wave * X::kRow + i * 1024);
-                load_to_lds_16(v_rows, at_row + (v_piece ^ (32 * i)), slot + X::kK + 8 * wave * X::kRow + i * 1024);
+                auto* const v = reinterpret_cast<__attribute__((address_space(3))) s16x8*>(lds + at_v + 1024 * i);
+                s16x8 y = *v;
+                bool odd = false;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if ((y[e] & 0x7C00) == 0x7C00) {
+                        odd = true;
+                        y[e] = 0;
+                    }
+                if (odd) {
+                    *v = y;
+                    *s_odd = 1;
+                }
             }
-            load_to_lds_16(x.a, number(lane >> 3) * static_cast<unsigned>(2 * L) + r_piece, slot + 2 * X::kK + 8 * wave * 2 * kRope);
         };
 
         // ---- the wave's rows of Q, times a power of two that brings the largest of a row to [2^8, 2^9) ----
@@ -369,10 +392,17 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
         }
         wait_vm_all();
         load_row_numbers(1);
-        issue(0);
-        if (steps > 1) issue(1);
-        if (steps > 1) wait_vm<kLoads>();
+        issue_k(0, 0);
+        issue_v(0, 0);
+        if (steps > 1) issue_k(1, X::kSlot);
+        if (steps > 1) issue_v(1, X::kSlot);
+        if (steps > 2) issue_k(2, 2 * X::kSlot);
+        if (steps > 2) wait_vm<kLoads>();
+        else if (steps > 1) wait_vm<kRowLoads>();
         else wait_vm_all();
+        if (tid == 0) *s_odd = 0;
+        lds_barrier();
+        clean(0, 0);
         lds_barrier();
 
         const bool head = k0 == 0, last = k1 == all_steps, whole = head && last;
@@ -381,44 +411,71 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
         // The tile, with keys and values as they are (the usual case) or with powers of two of their own.
         auto walk = [&](auto scaled_c) __attribute__((always_inline)) {
             constexpr bool scaled = decltype(scaled_c)::value;
-            f32x4 sc[2][RB];
+            f32x4 sc[2][RB], next[2][RB];  // scores of this step and of the one behind it
+            float m[RB], l[RB];
+            bool fresh = true, flushed = false;  // fresh: no maxima yet
             // the power of two of a key's or value's block
             auto exponent = [&](const signed char* of, int j) -> int {
-                return j >= key_end ? 0 : of[copy * (x.rows_cap / kBlockRows) + (j < P ? row_of[j] : e0 + (j - P)) / kBlockRows];
+                return j >= key_end ? 0 : of[copy * (x.rows_cap / kBlockRows) + row_of[j] / kBlockRows];
             };
-            auto scores = [&](int rel) __attribute__((always_inline)) {
-                const unsigned slot = (rel % kExpSlots) * X::kSlot;
-                const int j0 = (k0 + rel) * kExpStep;
+            // a quarter of the probabilities of the scores of step rel, [rb][kb], and their sums
+            f16x8 pr[RB];
+            unsigned pw[RB][4];
+            float sum[RB];
+            auto probabilities = [&](int rel, int kb, int rb) __attribute__((always_inline)) {
+                float p[4];
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) sc[kb][rb] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int s = 0; s < KS; ++s)
-#pragma unroll
-                    for (int kb = 0; kb < 2; ++kb) {
-                        const f16x8 kf = *reinterpret_cast<__attribute__((address_space(3))) const f16x8*>(lds + (k_at[s] + slot) + kb * 16 * X::kRow);
-#pragma unroll
-                        for (int rb = 0; rb < RB; ++rb) sc[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q[rb][s], sc[kb][rb], 0, 0, 0);
-                    }
-                if constexpr (scaled) {
-#pragma unroll
-                    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float by = power_of_two(exponent(x.k_exp, j0 + 16 * kb + 4 * g4 + i));
-#pragma unroll
-                            for (int rb = 0; rb < RB; ++rb) sc[kb][rb][i] *= by;
-                        }
+                for (int i = 0; i < 4; ++i) {
+                    p[i] = __builtin_amdgcn_exp2f(fmaf(sc[kb][rb][i], c[rb], -m[rb]));
+                    sum[rb] += p[i];
+                    if constexpr (scaled) p[i] *= power_of_two(max(exponent(x.v_exp, (k0 + rel) * kExpStep + 16 * kb + 4 * g4 + i) - x.v_top[h], -126));
                 }
+                pw[rb][2 * kb] = worked_out_here(pack_f16x2(p[0], p[1]));  // (here, and not where it is used)
+                pw[rb][2 * kb + 1] = worked_out_here(pack_f16x2(p[2], p[3]));
+            };
+            // The scores of step rel + 1 into `next`, and beside them the probabilities of step rel: a piece of these behind every few products.
+            // Fragments are read four ahead.
+            constexpr int kFrags = 2 * (KS + KSR), kAhead = 4;
+            auto scores = [&](int rel1, unsigned slot, auto with) __attribute__((always_inline)) {
+                constexpr bool probs = decltype(with)::value;
 #pragma unroll
-                for (int s = 0; s < KSR; ++s)
+                for (int rb = 0; rb < RB; ++rb) sum[rb] = 0.f;
+                const int j0 = (k0 + rel1) * kExpStep;
+                u32x4 kf[kFrags];
+                auto read = [&](int f) __attribute__((always_inline)) {
+                    const int s = f >> 1, kb = f & 1;
+                    kf[f] = *reinterpret_cast<__attribute__((address_space(3))) const u32x4*>(
+                        lds + (s < KS ? k_at[s] + kb * 16 * X::kRow : r_at[s - KS] + kb * 16 * 2 * kRope) + slot);
+                };
 #pragma unroll
-                    for (int kb = 0; kb < 2; ++kb) {
-                        const bf16x8 kf = *reinterpret_cast<__attribute__((address_space(3))) const bf16x8*>(lds + (r_at[s] + slot) + kb * 16 * 2 * kRope);
+                for (int f = 0; f < kAhead; ++f) read(f);
+                in_this_order();
 #pragma unroll
-                        for (int rb = 0; rb < RB; ++rb) sc[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qr[rb][s], sc[kb][rb], 0, 0, 0);
+                for (int f = 0; f < kFrags; ++f) {
+                    const int s = f >> 1, kb = f & 1;
+                    if (scaled && f == 2 * KS) {
+#pragma unroll
+                        for (int y = 0; y < 2; ++y)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float by = power_of_two(exponent(x.k_exp, j0 + 16 * y + 4 * g4 + i));
+#pragma unroll
+                                for (int rb = 0; rb < RB; ++rb) next[y][rb][i] *= by;
+                            }
                     }
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) {
+                        const f32x4 before = s == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : next[kb][rb];
+                        if (s < KS) next[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, kf[f]), q[rb][s < KS ? s : 0], before, 0, 0, 0);
+                        else next[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[f]), qr[rb][s < KS ? 0 : s - KS], before, 0, 0, 0);
+                    }
+                    if (f + kAhead < kFrags) read(f + kAhead);
+                    if constexpr (probs) {
+                        constexpr int kEvery = kFrags / 4;
+                        if (f % kEvery == 0 && f / kEvery < 4) probabilities(rel1 - 1, (f / kEvery) & 1, (f / kEvery) >> 1);
+                    }
+                    in_this_order();
+                }
                 if (j0 + kExpStep > vis_min) {
 #pragma unroll
                     for (int rb = 0; rb < RB; ++rb) {
@@ -427,12 +484,10 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
                         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                             for (int i = 0; i < 4; ++i)
-                                if (16 * kb + i >= sees) sc[kb][rb][i] = -INFINITY;
+                                if (16 * kb + i >= sees) next[kb][rb][i] = -INFINITY;
                     }
                 }
             };
-            float m[RB], l[RB];
-            bool fresh = true, flushed = false, odd_seen = false;  // fresh: no maxima yet, the wave has seen no key
             auto largest = [&](int rb) __attribute__((always_inline)) {
                 float mx = sc[0][rb][0];
 #pragma unroll
@@ -441,54 +496,32 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
                     for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[kb][rb][i]);
                 return mx * c[rb];
             };
-            f16x8 pr[RB];
-            auto probabilities = [&](int rel) __attribute__((always_inline)) {
-                float by[2][4];
-                if constexpr (scaled) {
-                    const int v_top = x.v_top[h];
+            auto take_next = [&]() __attribute__((always_inline)) {
 #pragma unroll
-                    for (int kb = 0; kb < 2; ++kb)
+                for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) by[kb][i] = power_of_two(max(exponent(x.v_exp, (k0 + rel) * kExpStep + 16 * kb + 4 * g4 + i) - v_top, -126));
-                }
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb) {
-                    float p[2][4];
-#pragma unroll
-                    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            p[kb][i] = __builtin_amdgcn_exp2f(fmaf(sc[kb][rb][i], c[rb], -m[rb]));
-                            l[rb] += p[kb][i];
-                            if constexpr (scaled) p[kb][i] *= by[kb][i];
-                        }
-                    pr[rb] = __builtin_bit_cast(f16x8, make_uint4(pack_f16x2(p[0][0], p[0][1]), pack_f16x2(p[0][2], p[0][3]), pack_f16x2(p[1][0], p[1][1]),
-                                                                  pack_f16x2(p[1][2], p[1][3])));
-                }
+                    for (int rb = 0; rb < RB; ++rb) sc[kb][rb] = next[kb][rb];
             };
-            auto output = [&](int rel, f32x4 (&o)[RB][NB], auto masked) __attribute__((always_inline)) {
-                const unsigned slot = (rel % kExpSlots) * X::kSlot, v_here = worked_out_here(v_at);
+            auto output = [&](unsigned slot, f32x4 (&o)[RB][NB]) __attribute__((always_inline)) {
+                const unsigned v_here = worked_out_here(v_at);
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) pr[rb] = __builtin_bit_cast(f16x8, u32x4{pw[rb][0], pw[rb][1], pw[rb][2], pw[rb][3]});
+                s16x4 vf[NB][2];
+                auto read = [&](int cb) __attribute__((always_inline)) {
+                    const unsigned a = (v_here ^ (32 * cb)) + slot;
+                    vf[cb][0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + a));
+                    vf[cb][1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + a + 16 * X::kRow));
+                };
+#pragma unroll
+                for (int cb = 0; cb < 3; ++cb) read(cb);
+                in_this_order();
 #pragma unroll
                 for (int cb = 0; cb < NB; ++cb) {
-                    const unsigned a = (v_here ^ (32 * cb)) + slot;
-                    s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + a));
-                    s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + a + 16 * X::kRow));
-                    s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                    if constexpr (decltype(masked)::value) {
-                        // 0 times an infinity or NaN of a key that some row does not see would be NaN: such values are given to the rows that see
-                        // them at the end instead
-                        bool odd = false;
+                    const f16x8 v = __builtin_bit_cast(f16x8, __builtin_shufflevector(vf[cb][0], vf[cb][1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if ((v[e] & 0x7C00) == 0x7C00) {
-                                odd = true;
-                                v[e] = 0;
-                            }
-                        if (__any(odd)) odd_seen = true;
-                    }
-                    const f16x8 vf = __builtin_bit_cast(f16x8, v);
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) o[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pr[rb], o[rb][cb], 0, 0, 0);
+                    for (int rb = 0; rb < RB; ++rb) o[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pr[rb], o[rb][cb], 0, 0, 0);
+                    if (cb + 3 < NB) read(cb + 3);
+                    in_this_order();
                 }
             };
             // scratch memory of the wave, this lane's part: row 16 rb + n, columns 16 cb + 4 g4 .. + 3
@@ -500,38 +533,40 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
             for (int rb = 0; rb < RB; ++rb) m[rb] = l[rb] = 0.f;
             int rel = 0;
             f32x4 o[RB][NB];
+            unsigned slot = 0;  // of step rel; the two behind it
+            auto behind = [](unsigned x) { return x == 2 * X::kSlot ? 0u : x + X::kSlot; };
+            scores(0, 0, std::false_type{});
+            take_next();
+            bool grown = true;
             while (true) {
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
                     for (int cb = 0; cb < NB; ++cb) o[rb][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
-                bool grown = false;
-                while (rel < steps) {
-                    const int j0 = (k0 + rel) * kExpStep;
-                    const bool on = j0 < vis_max;  // (a wave whose rows see none of these keys only loads)
-                    if (on) {
-                        scores(rel);
-                        bool outgrown = fresh;
+                while (rel < steps && !grown) {
+                    const unsigned slot1 = behind(slot), slot2 = behind(slot1);
+                    scores(rel + 1, slot1, std::true_type{});  // (behind the last step: of whatever lies there, not used)
+                    bool outgrown = false;
 #pragma unroll
-                        for (int rb = 0; rb < RB; ++rb) outgrown |= largest(rb) - m[rb] > kExpGrow;
-                        if (__any(outgrown)) {
-                            grown = true;
-                            break;
-                        }
-                    }
+                    for (int rb = 0; rb < RB; ++rb) outgrown |= sum[rb] > kExpMost;
+                    grown = __any(outgrown);
+                    if (grown) break;
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) l[rb] += sum[rb];
                     if ((rel & 7) == 6) load_row_numbers((rel + 2) / 8 + 1);
-                    if (rel + 2 < steps) issue(rel + 2);
-                    if (on) {
-                        probabilities(rel);
-                        if (j0 + kExpStep <= vis_min) output(rel, o, std::false_type{});
-                        else output(rel, o, std::true_type{});
-                    }
-                    if (rel + 2 < steps) wait_vm<kLoads>();
+                    if (rel + 2 < steps) issue_v(rel + 2, slot2);
+                    if (rel + 3 < steps) issue_k(rel + 3, slot);
+                    output(slot, o);
+                    take_next();
+                    if (rel + 3 < steps) wait_vm<kLoads>();
+                    else if (rel + 2 < steps) wait_vm<kRowLoads>();
                     else wait_vm_all();
+                    if (rel + 1 < steps) clean(rel + 1, slot1);
                     lds_barrier();
+                    slot = slot1;
                     ++rel;
                 }
-                if (!grown) break;
+                if (rel >= steps) break;
                 {
                     // new maxima, from the scores at hand; what has been summed up moves to memory, multiplied accordingly
 #pragma unroll
@@ -552,13 +587,14 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
                         m[rb] = mn;
                     }
                     if (!fresh) flushed = true;
-                    fresh = false;
+                    fresh = grown = false;
                 }
             }
 
             // ---- the end of the tile, or of the workgroup's part of it ----
             const unsigned lane_now = worked_out_here(lane);
             const int n = lane_now & 15, g4 = lane_now >> 4;
+            const bool odd_seen = __builtin_amdgcn_readfirstlane(*s_odd) != 0;
             const float back = scaled ? power_of_two(x.v_top[h]) : 1.f;
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
@@ -575,9 +611,9 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
                     if constexpr (scaled) y *= back;
                     const int col = 16 * cb + 4 * g4;
                     if (odd_seen) {
-                        // (a weight is positive: an infinity stays one, two of opposite sign and NaN give NaN; the keys of the blocks they were taken out of)
-                        for (int j = max(vis_min & ~(kExpStep - 1), k0 * kExpStep); j < min(P + row0 + row + 1, k1 * kExpStep); ++j) {
-                            const int64_t at_row = j < P ? row_of[j] : e0 + (j - P);
+                        // (a weight is positive: an infinity stays one, two of opposite sign and NaN give NaN; the keys of the steps they were taken out of)
+                        for (int j = max((P + row0 + 1) & ~(kExpStep - 1), k0 * kExpStep); j < min(P + row0 + row + 1, k1 * kExpStep); ++j) {
+                            const int64_t at_row = row_of[j];
                             const unsigned short* const v4 = reinterpret_cast<const unsigned short*>(v_rows) + at_row * N + col;
 #pragma unroll
                             for (int i = 0; i < 4; ++i)
@@ -597,6 +633,7 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
             used[head ? 1 : 0] = true;
             if (tid == 0) parts.rec[part] = make_int4(out_row0, rows_here, (head ? kPartHead : 0) | (last ? kPartLast : 0), H);
         }
+        lds_barrier();  // (nobody looks at the flag any more)
         ++at.tile;
         at.k = 0;
         if (k1 != all_steps) break;

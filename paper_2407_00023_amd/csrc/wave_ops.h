@@ -89,6 +89,9 @@ __device__ __forceinline__ unsigned worked_out_here(unsigned x) {
     asm volatile("" : "+v"(x));
     return x;
 }
+// Nothing is moved across this place: what is written before it is issued before it.  (Left to itself the compiler reads one fragment at a time
+// from LDS, waits, and multiplies.)
+__device__ __forceinline__ void in_this_order() { __builtin_amdgcn_sched_barrier(0); }
 // s_waitcnt vmcnt(N): all but the newest N of the wave's loads have landed.
 template <int N>
 __device__ __forceinline__ void wait_vm() {
