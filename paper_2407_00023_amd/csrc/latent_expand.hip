@@ -31,7 +31,7 @@ typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr size_t kExpandedBytes = size_t{1} << 30;
+constexpr size_t kExpandedBytes = size_t{4} << 30;
 constexpr int kExpandWorkgroups = 256;  // one on a compute unit
 constexpr int kExpWorkgroups = 512;     // two
 constexpr int kExpM = 128;           // rows of q of a tile
@@ -144,10 +144,34 @@ __global__ __launch_bounds__(256, 1) void latent_expand_kernel(ExpandArgs x, con
     const int wg = blockIdx.x;
     int64_t unit = units * wg / gridDim.x;
     const int64_t end = units * (wg + 1) / gridDim.x;
+    // A unit's rows of A are asked for kAhead slices of 32 values ahead, the first of the next unit's beside the last products of this one's.
+    constexpr int kAhead = 4;
+    auto row_of_unit = [&](int64_t u) { return (u % blocks) * 256 + 64 * wave; };
+    const uint4* from[4];
+    auto point_at = [&](int64_t u) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) from[r] = reinterpret_cast<const uint4*>(x.a + min(row_of_unit(u) + 16 * r + n, rows - 1) * L) + 2 * g4;
+    };
+    // (a lane takes 32 bytes behind one another for two slices, so that a line of memory is used at once; the order of a sum's terms is free)
+    u32x4 af[kAhead][4];
+    auto fetch_two = [&](int s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) af[(s + t) % kAhead][r] = __builtin_bit_cast(u32x4, from[r][4 * s + t]);
+    };
+    unsigned w_at[4];  // LDS address of a fragment of W, by its slice mod 4
+#pragma unroll
+    for (int s = 0; s < 4; ++s) w_at[s] = n * 2 * R + 16 * ((8 * (s >> 1) + 2 * g4 + (s & 1)) ^ n);
     int have = -1;
+    if (unit < end) {
+        point_at(unit);
+#pragma unroll
+        for (int s = 0; s < kAhead; s += 2) fetch_two(s);
+    }
     for (; unit < end; ++unit) {
         const int set = static_cast<int>(unit / blocks), h = set / kSets;
-        const int64_t row0 = (unit - set * blocks) * 256 + 64 * wave;
+        const int64_t row0 = row_of_unit(unit);
         if (set != have) {
             have = set;
             lds_barrier();  // (nobody reads the old columns any more)
@@ -155,8 +179,8 @@ __global__ __launch_bounds__(256, 1) void latent_expand_kernel(ExpandArgs x, con
             for (int i = wave; i < 128 / kRowsPerLoad; i += 4) {
                 const int row = i * kRowsPerLoad + lane / (64 / kRowsPerLoad);
                 const int col = (set % kSets) * 128 + row;  // among the head's 2 N
-                const __hip_bfloat16* const from = (col < N ? w_k : w_v) + (static_cast<int64_t>(h0 + h) * N + (col < N ? col : col - N)) * R;
-                load_to_lds_16(from + 8 * ((lane & (64 / kRowsPerLoad - 1)) ^ (row & 15)), lds0 + i * 1024);
+                const __hip_bfloat16* const w = (col < N ? w_k : w_v) + (static_cast<int64_t>(h0 + h) * N + (col < N ? col : col - N)) * R;
+                load_to_lds_16(w + 8 * ((lane & (64 / kRowsPerLoad - 1)) ^ (row & 15)), lds0 + i * 1024);
             }
             wait_vm_all();
             lds_barrier();
@@ -166,19 +190,26 @@ __global__ __launch_bounds__(256, 1) void latent_expand_kernel(ExpandArgs x, con
         for (int c = 0; c < 8; ++c)
 #pragma unroll
             for (int r = 0; r < 4; ++r) acc[c][r] = f32x4{0.f, 0.f, 0.f, 0.f};
-        const uint4* from[4];
+        constexpr int kWAhead = 3;
+        u32x4 wf[kWAhead + 1];
+        auto read = [&](int f) __attribute__((always_inline)) {
+            const int s = f >> 3, c = f & 7;
+            wf[f % (kWAhead + 1)] = *reinterpret_cast<__attribute__((address_space(3))) const u32x4*>(lds + w_at[s & 3] + c * 16 * 2 * R + (s >> 2) * 256);
+        };
 #pragma unroll
-        for (int r = 0; r < 4; ++r) from[r] = reinterpret_cast<const uint4*>(x.a + min(row0 + 16 * r + n, rows - 1) * L) + g4;
+        for (int f = 0; f < kWAhead; ++f) read(f);
+        in_this_order();
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-            bf16x8 af[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) af[r] = __builtin_bit_cast(bf16x8, from[r][4 * s]);
+            if (s + kAhead == KS) point_at(min(unit + 1, end - 1));  // (KS, kAhead: even)
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
-                const bf16x8 wf = *reinterpret_cast<__attribute__((address_space(3))) const bf16x8*>(lds + (16 * c + n) * 2 * R + 16 * ((4 * s + g4) ^ n));
+                if (s * 8 + c + kWAhead < KS * 8) read(s * 8 + c + kWAhead);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, af[r], acc[c][r], 0, 0, 0);
+                for (int r = 0; r < 4; ++r)
+                    acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wf[(s * 8 + c) % (kWAhead + 1)]), __builtin_bit_cast(bf16x8, af[s % kAhead][r]), acc[c][r], 0, 0, 0);
+                if (c == 7 && (s & 1)) fetch_two((s - 1 + kAhead) % KS);
+                in_this_order();
             }
         }
         // lane: row 16 r + n, columns 16 c + 4 g4 .. + 3
@@ -192,15 +223,28 @@ __global__ __launch_bounds__(256, 1) void latent_expand_kernel(ExpandArgs x, con
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float y = fabsf(acc[c][r][i]);
-                        if (row0 + 16 * r + n < rows && y < INFINITY) top = fmaxf(top, y);
-                    }
+                    for (int i = 0; i < 4; ++i) top = fmaxf(top, fabsf(acc[c][r][i]));  // (rows behind the last are copies of it)
+            if (__any(top == INFINITY)) {  // (of the finite ones)
+                top = 0.f;
+#pragma unroll
+                for (int c = part * CK; c < (part + 1) * CK; ++c)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (fabsf(acc[c][r][i]) < INFINITY) top = fmaxf(top, fabsf(acc[c][r][i]));
+            }
 #pragma unroll
             for (int off = 1; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
             int e = 0;
             if (top != 0.f && !(top >= 0.015625f && top < 32768.f)) e = max(min(static_cast<int>(__float_as_uint(top) >> 23) - 127 - 13, 126), -126);
-            const float by = power_of_two(-e);
+            if (e != 0) {
+                const float by = power_of_two(-e);
+#pragma unroll
+                for (int c = part * CK; c < (part + 1) * CK; ++c)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[c][r] *= by;
+            }
             if (row0 < rows && lane == 0) {
                 (is_v ? x.v_exp : x.k_exp)[h * (x.rows_cap / kBlockRows) + row0 / kBlockRows] = static_cast<signed char>(e);
                 if (e != 0) atomicOr(&x.scaled[h0 + h], 1);
@@ -213,7 +257,7 @@ __global__ __launch_bounds__(256, 1) void latent_expand_kernel(ExpandArgs x, con
 #pragma unroll
                     for (int c = part * CK; c < (part + 1) * CK; ++c)
                         *reinterpret_cast<uint2*>(to + (16 * r + n) * N + (c - part * CK) * 16 + 4 * g4) =
-                            make_uint2(pack_f16x2(acc[c][r][0] * by, acc[c][r][1] * by), pack_f16x2(acc[c][r][2] * by, acc[c][r][3] * by));
+                            make_uint2(pack_f16x2(acc[c][r][0], acc[c][r][1]), pack_f16x2(acc[c][r][2], acc[c][r][3]));
         }
     }
 }

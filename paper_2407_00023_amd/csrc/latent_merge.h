@@ -8,34 +8,63 @@
 
 namespace pa {
 
-// The parts of a tile joined: workgroup (w, y) of the launch takes the tile that workgroup w of the attention began and did not finish, if there
-// is one, and kJoinRows of its rows.
-constexpr int kJoinRows = 4;
+// The parts of tiles joined.  Every workgroup looks at all records, 512 at most, and counts what there is to join, in pieces of kJoinRows rows; the
+// pieces are dealt out in turn.  (A workgroup for every piece that there could be took 40 us to find that most of it had nothing to do.)
+constexpr int kMergeGroups = 2048;  // eight on a compute unit
+constexpr int kMaxParts = 512;
 template <int R>
-__global__ __launch_bounds__(256) void latent_merge_kernel(LatentParts parts, int M, __hip_bfloat16* __restrict__ out) {
-    constexpr int kCols = R / 4, kRowsAtOnce = 256 / kCols;  // threads of a row
-    __shared__ float s_w[512][kJoinRows];
-    const int w = blockIdx.x, n = parts.hdr[6];
-    if (w >= n) return;
-    const int4 rec = parts.rec[2 * w + 1];
-    const int row0 = blockIdx.y * kJoinRows;
-    if (!(rec.z & kPartHead) || row0 >= rec.y) return;
-    // parts: slot 2 w + 1, then 2 (w + 1), 2 (w + 2), ... up to the one that ends the tile
-    const int tid = threadIdx.x, lane = tid & 63;
-    int count = 1;
-    for (bool more = true; more;) {
-        const int i = w + count + lane;
-        const int flags = i < n ? parts.rec[2 * i].z : kPartLast;
-        const unsigned long long ends = __ballot(flags & kPartLast);
-        count += ends ? __builtin_ctzll(ends) + 1 : 64;
-        more = ends == 0;
+__global__ __launch_bounds__(256) void latent_merge_kernel(LatentParts parts, int M, int n_max, __hip_bfloat16* __restrict__ out) {
+    constexpr int kCols = R / 4, kRowsAtOnce = 256 / kCols, kJoinRows = kRowsAtOnce > 4 ? kRowsAtOnce : 4;  // threads of a row
+    __shared__ int s_last[kMaxParts], s_sum[4], s_found[2];
+    __shared__ float s_w[kMaxParts][kJoinRows];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = parts.hdr[6];
+    int pieces[2], before[2];
+    int4 rec[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int w = 2 * tid + i;
+        rec[i] = w < n_max ? parts.rec[2 * w + 1] : make_int4(0, 0, 0, 0);
+        s_last[w] = w < n_max ? parts.rec[2 * w].z & kPartLast : kPartLast;
+        pieces[i] = w < n && (rec[i].z & kPartHead) ? (rec[i].y + kJoinRows - 1) / kJoinRows : 0;
     }
-    auto slot = [&](int p) { return p == 0 ? 2 * w + 1 : 2 * (w + p); };
-    const int rows = min(kJoinRows, rec.y - row0);
-    // weights of the parts: 2^(their maximum - the largest) over the sum
-    if (tid < 64 * kJoinRows) {
-        const int row = tid >> 6;
-        if (row < rows) {
+    int in = pieces[0] + pieces[1];
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const int y = __shfl_up(in, off);
+        if (lane >= off) in += y;
+    }
+    if (lane == 63) s_sum[wave] = in;
+    __syncthreads();
+    int all = 0;
+    for (int w = 0; w < 4; ++w) {
+        if (w < wave) in += s_sum[w];
+        all += s_sum[w];
+    }
+    before[0] = in - pieces[0] - pieces[1];
+    before[1] = before[0] + pieces[0];
+    for (int piece = blockIdx.x; piece < all; piece += gridDim.x) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (before[i] <= piece && piece < before[i] + pieces[i]) {
+                s_found[0] = 2 * tid + i;
+                s_found[1] = piece - before[i];
+            }
+        __syncthreads();
+        const int w = __builtin_amdgcn_readfirstlane(s_found[0]), row0 = __builtin_amdgcn_readfirstlane(s_found[1]) * kJoinRows;
+        const int4 r = parts.rec[2 * w + 1];
+        const int here = min(kJoinRows, r.y - row0);
+        // parts: slot 2 w + 1, then 2 (w + 1), 2 (w + 2), ... up to the one that ends the tile
+        int count = 1;
+        for (bool more = true; more;) {
+            const int i = w + count + lane;
+            const unsigned long long ends = __ballot(i < n ? s_last[i] : 1);
+            count += ends ? __builtin_ctzll(ends) + 1 : 64;
+            more = ends == 0;
+        }
+        count = min(count, n_max - w);
+        auto slot = [&](int p) { return p == 0 ? 2 * w + 1 : 2 * (w + p); };
+        // weights of the parts: 2^(their maximum - the largest) over the sum
+        for (int row = wave; row < here; row += 4) {
             float mx = -INFINITY, sum = 0.f;
             for (int p = lane; p < count; p += 64) {
                 const float2 ml = parts.ml[static_cast<size_t>(slot(p)) * M + row0 + row];
@@ -54,33 +83,34 @@ __global__ __launch_bounds__(256) void latent_merge_kernel(LatentParts parts, in
             for (int off = 1; off < 64; off <<= 1) sum += __shfl_xor(sum, off);
             for (int p = lane; p < count; p += 64) s_w[p][row] /= sum;
         }
-    }
-    __syncthreads();
-    const int c = tid % kCols;
-    for (int row = tid / kCols; row < rows; row += kRowsAtOnce) {
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int p = 0; p < count; ++p) {
-            const float a = s_w[p][row];
-            const float4 v = *reinterpret_cast<const float4*>(parts.o + (static_cast<size_t>(slot(p)) * M + row0 + row) * R + 4 * c);
-            if (a != 0.f) {
-                acc.x += a * v.x;
-                acc.y += a * v.y;
-                acc.z += a * v.z;
-                acc.w += a * v.w;
+        __syncthreads();
+        const int c = tid % kCols;
+        for (int row = tid / kCols; row < here; row += kRowsAtOnce) {
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+            for (int p = 0; p < count; ++p) {
+                const float a = s_w[p][row];
+                const float4 v = *reinterpret_cast<const float4*>(parts.o + (static_cast<size_t>(slot(p)) * M + row0 + row) * R + 4 * c);
+                if (a != 0.f) {
+                    acc.x += a * v.x;
+                    acc.y += a * v.y;
+                    acc.z += a * v.z;
+                    acc.w += a * v.w;
+                }
             }
+            *reinterpret_cast<uint2*>(out + (r.x + static_cast<int64_t>(row0 + row) * r.w) * R + 4 * c) = make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
         }
-        *reinterpret_cast<uint2*>(out + (rec.x + static_cast<int64_t>(row0 + row) * rec.w) * R + 4 * c) = make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
+        __syncthreads();
     }
 }
 
 inline void launch_latent_merge(const LatentParts& parts, int n_wg, int M, int width, void* out, hipStream_t stream) {
-    const dim3 grid(n_wg, M / kJoinRows);
+    const dim3 grid(kMergeGroups);
     __hip_bfloat16* const o = static_cast<__hip_bfloat16*>(out);
-    if (width == 512) hipLaunchKernelGGL(latent_merge_kernel<512>, grid, dim3(256), 0, stream, parts, M, o);
-    else if (width == 256) hipLaunchKernelGGL(latent_merge_kernel<256>, grid, dim3(256), 0, stream, parts, M, o);
-    else if (width == 128) hipLaunchKernelGGL(latent_merge_kernel<128>, grid, dim3(256), 0, stream, parts, M, o);
-    else hipLaunchKernelGGL(latent_merge_kernel<64>, grid, dim3(256), 0, stream, parts, M, o);
+    if (width == 512) hipLaunchKernelGGL(latent_merge_kernel<512>, grid, dim3(256), 0, stream, parts, M, n_wg, o);
+    else if (width == 256) hipLaunchKernelGGL(latent_merge_kernel<256>, grid, dim3(256), 0, stream, parts, M, n_wg, o);
+    else if (width == 128) hipLaunchKernelGGL(latent_merge_kernel<128>, grid, dim3(256), 0, stream, parts, M, n_wg, o);
+    else hipLaunchKernelGGL(latent_merge_kernel<64>, grid, dim3(256), 0, stream, parts, M, n_wg, o);
 }
 
 }  // namespace pa
