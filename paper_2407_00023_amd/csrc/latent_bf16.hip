@@ -39,7 +39,7 @@ typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kStep = 32;       // keys of a step
-constexpr float kGrow = 40.f;  // log2 units
+constexpr float kMost = 1099511627776.f;  // 2^40
 
 __device__ const uint4 g_zero_row[128] = {};  // stands for keys behind the last one of a tile
 
@@ -103,6 +103,8 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
         const int piece = (16 * NB * wave >> 3) + ((n & 3) >> 1);
         v_at = row * X::kLatRow + 16 * (piece ^ swz(row & 15)) + 8 * (n & 1);
     }
+    // (probabilities: 64 bytes a row, in pieces of 16; the second block of 16 keys by XOR)
+    const unsigned p_wr = X::kProbAt + (wrow + n) * 64 + 16 * (((wkey >> 3) + (g4 >> 1)) ^ (n >> 2)) + 8 * (g4 & 1);
     const unsigned p_rd = X::kProbAt + n * 64 + 16 * (g4 ^ (n >> 2));
 
     bool used[2] = {false, false};  // partial results left in this workgroup's two slots
@@ -142,10 +144,11 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
                 load_to_lds_4(slots + min(j, P - 1), lds0 + X::kSlotsAt + wave * 512 + (blk & 1) * 256);
             }
         };
-        auto issue = [&](int rel) {
+        auto issue = [&](int rel, int lat_slot, int rope_slot) __attribute__((always_inline)) {
             const int j0 = (k0 + rel) * kStep + 8 * wave;
             const int* const sl = s_slots + ((rel >> 3) & 1) * 64 + (rel & 7) * 8;
-            const unsigned lat = lds0 + (rel % X::kLatSlots) * X::kLat + 8 * wave * X::kLatRow, rope = lds0 + X::kRopeAt + (rel % X::kRopeSlots) * X::kRopeStep + 8 * wave * 2 * kRope;
+            [[maybe_unused]] const unsigned lat = lds0 + lat_slot * X::kLat + 8 * wave * X::kLatRow;
+            const unsigned rope = lds0 + X::kRopeAt + rope_slot * X::kRopeStep + 8 * wave * 2 * kRope;
             if constexpr (!KV8 && RPL == 1) {
                 const uint64_t a = row_address(j0 + (lane & 7), sl[lane & 7]);
                 const unsigned lo = static_cast<unsigned>(a), hi = static_cast<unsigned>(a >> 32);
@@ -184,9 +187,9 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
         // 8-bit pool.  All rows of a step are in the pool: its loads are kLoads, no row goes to its place in LDS directly.
         auto pure = [&](int rel) { return !KV8 || (k0 + rel + 1) * kStep <= P; };
         // rows that are bf16 in memory (extend tokens, and what stands for keys behind the last), to their place
-        auto issue_direct = [&](int rel) {
+        auto issue_direct = [&](int rel, int lat_slot) {
             const int j0 = (k0 + rel) * kStep + 8 * wave;
-            const unsigned lat = lds0 + (rel % X::kLatSlots) * X::kLat + 8 * wave * X::kLatRow;
+            const unsigned lat = lds0 + lat_slot * X::kLat + 8 * wave * X::kLatRow;
 #pragma unroll
             for (int i = 0; i < 8 / RPL; ++i) {
                 const int row = i * RPL + lane / (64 / RPL);
@@ -196,10 +199,10 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
             }
         };
         // codes that landed, to bf16 rows (the wave's own)
-        auto convert = [&](int rel) {
+        auto convert = [&](int rel, int lat_slot) __attribute__((always_inline)) {
             const int j0 = (k0 + rel) * kStep + 8 * wave;
             const unsigned from = X::kCodesAt + (rel & 1) * X::kCodes + 8 * wave * R, exps = X::kExpAt + wave * 64 + (rel & 1) * 32;
-            const unsigned to = (rel % X::kLatSlots) * X::kLat + 8 * wave * X::kLatRow;
+            const unsigned to = lat_slot * X::kLat + 8 * wave * X::kLatRow;
 #pragma unroll
             for (int i = 0; i < 8 / RPL; ++i) {
                 const int row = i * RPL + lane / (64 / RPL), piece = lane & (64 / RPL - 1);
@@ -228,41 +231,63 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
         float m[RW], l[RW];
 #pragma unroll
         for (int rb = 0; rb < RW; ++rb) m[rb] = l[rb] = 0.f;
-        if (tid < 2) s_flag[tid] = -1;
+        if (tid < 3) s_flag[tid] = tid < 2 ? -1 : 0;
         wait_vm_all();
         load_slots(1);
-        issue(0);
-        if (steps > 1) issue(1);
-        if (!KV8 && steps > 2) issue(2);
+        issue(0, 0, 0);
+        if (steps > 1) issue(1, 1, 1);
+        if (!KV8 && steps > 2) issue(2, 2, 2);
         if (KV8) {
-            if (!pure(0)) issue_direct(0);
-            if (steps > 1 && !pure(1)) issue_direct(1);
+            if (!pure(0)) issue_direct(0, 0);
+            if (steps > 1 && !pure(1)) issue_direct(1, 1);
         }
 
         // ---- the pieces of an interval ----
+        // Keys that some row of the tile does not see may hold an infinity or NaN, and 0 times that is NaN: before the output of a step with such keys, when
+        // its scores are done, the wave that loaded a row takes such values out of it; the end of the tile gives them to the rows that see them.
+        auto has_hidden = [&](int rel) { return vis_min < key_end && (k0 + rel + 1) * kStep > vis_min; };
+        auto clean = [&](int lat_slot) {
+            const unsigned at_row = lat_slot * X::kLat + 8 * wave * X::kLatRow + 16 * lane;
+#pragma unroll
+            for (int i = 0; i < 8 / RPL; ++i) {
+                auto* const c8 = reinterpret_cast<__attribute__((address_space(3))) s16x8*>(lds + at_row + 1024 * i);
+                s16x8 y = *c8;
+                bool odd = false;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if ((y[e] & 0x7F80) == 0x7F80) {
+                        odd = true;
+                        y[e] = 0;
+                    }
+                if (odd) {
+                    *c8 = y;
+                    s_flag[2] = 1;
+                }
+            }
+        };
         f32x4 sc[KW][RW];
-        auto scores = [&](int rel) {
-            const unsigned lat = (rel % X::kLatSlots) * X::kLat, rope = (rel % X::kRopeSlots) * X::kRopeStep;
+        // Scores of a step; fragments are read kAhead ahead.
+        auto scores = [&](int rel, int lat_slot, int rope_slot) __attribute__((always_inline)) {
+            constexpr int kFrags = KW * (KS + KSR), kAhead = 4;
+            const unsigned lat = lat_slot * X::kLat, rope = rope_slot * X::kRopeStep;
+            u32x4 kf[kAhead + 1];
+            auto read = [&](int f) __attribute__((always_inline)) {
+                const int s = f / KW, kb = f % KW;
+                kf[f % (kAhead + 1)] = *reinterpret_cast<__attribute__((address_space(3))) const u32x4*>(
+                    s < KS ? lds + (k_at[s & 3] + lat) + kb * 16 * X::kLatRow + (s >> 2) * 256 : lds + (r_at[s < KS ? 0 : s - KS] + rope) + kb * 16 * 2 * kRope);
+            };
 #pragma unroll
-            for (int kb = 0; kb < KW; ++kb)
+            for (int f = 0; f < kAhead; ++f) read(f);
+            in_this_order();
 #pragma unroll
-                for (int rb = 0; rb < RW; ++rb) sc[kb][rb] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int f = 0; f < kFrags; ++f) {
+                const int s = f / KW, kb = f % KW;
+                if (f + kAhead < kFrags) read(f + kAhead);
 #pragma unroll
-            for (int s = 0; s < KS; ++s)
-#pragma unroll
-                for (int kb = 0; kb < KW; ++kb) {
-                    const bf16x8 kf = *reinterpret_cast<__attribute__((address_space(3))) const bf16x8*>(lds + (k_at[s & 3] + lat) + kb * 16 * X::kLatRow + (s >> 2) * 256);
-#pragma unroll
-                    for (int rb = 0; rb < RW; ++rb) sc[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[rb][s], sc[kb][rb], 0, 0, 0);
-                }
-#pragma unroll
-            for (int s = 0; s < KSR; ++s)
-#pragma unroll
-                for (int kb = 0; kb < KW; ++kb) {
-                    const bf16x8 kf = *reinterpret_cast<__attribute__((address_space(3))) const bf16x8*>(lds + (r_at[s] + rope) + kb * 16 * 2 * kRope);
-#pragma unroll
-                    for (int rb = 0; rb < RW; ++rb) sc[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[rb][KS + s], sc[kb][rb], 0, 0, 0);
-                }
+                for (int rb = 0; rb < RW; ++rb)
+                    sc[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[f % (kAhead + 1)]), q[rb][s], s == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sc[kb][rb], 0, 0, 0);
+                in_this_order();
+            }
             const int j0 = (k0 + rel) * kStep;
             if (j0 + kStep > vis_min) {
 #pragma unroll
@@ -274,23 +299,17 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
                             if (j0 + wkey + 16 * kb + 4 * g4 + i >= vis[rb]) sc[kb][rb][i] = -INFINITY;
             }
         };
-        // probabilities of the scores against the maxima as they stand, into buffer rel % 2; their sums
-        auto probabilities = [&](int rel) {
-            const unsigned to = X::kProbAt + (rel & 1) * X::kProb;
+        // a piece of the probabilities of the scores against the maxima as they stand, into buffer rel % 2; their sums
+        float sum[RW];
+        auto probabilities = [&](int rel, int kb, int rb) __attribute__((always_inline)) {
+            float p[4];
 #pragma unroll
-            for (int rb = 0; rb < RW; ++rb)
-#pragma unroll
-                for (int kb = 0; kb < KW; ++kb) {
-                    float p[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        p[i] = __builtin_amdgcn_exp2f(fmaf(sc[kb][rb][i], scale_log2e, -m[rb]));
-                        l[rb] += p[i];
-                    }
-                    const int piece = ((wkey + 16 * kb) >> 3) + (g4 >> 1);
-                    *reinterpret_cast<__attribute__((address_space(3))) u32x2*>(lds + to + (wrow + 16 * rb + n) * 64 + 16 * (piece ^ (n >> 2)) + 8 * (g4 & 1)) =
-                        u32x2{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3])};
-                }
+            for (int i = 0; i < 4; ++i) {
+                p[i] = __builtin_amdgcn_exp2f(fmaf(sc[kb][rb][i], scale_log2e, -m[rb]));
+                sum[rb] += p[i];
+            }
+            *reinterpret_cast<__attribute__((address_space(3))) u32x2*>(lds + ((p_wr + (rel & 1) * X::kProb + rb * 1024) ^ (kb * 32))) =
+                u32x2{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3])};
         };
         auto largest = [&](int rb) {
             float mx = sc[0][rb][0];
@@ -321,158 +340,176 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
                 const float mn = new_max(wrow + 16 * rb + n);
                 l[rb] = first ? 0.f : l[rb] * __builtin_amdgcn_exp2f(m[rb] - mn);
                 m[rb] = mn;
+                sum[rb] = 0.f;
             }
             const float mine = tid < M ? new_max(tid) : 0.f;
             lds_barrier();
             if (tid < M) s_max[tid] = mine;
-            probabilities(rel);
+#pragma unroll
+            for (int rb = 0; rb < RW; ++rb)
+#pragma unroll
+                for (int kb = 0; kb < KW; ++kb) probabilities(rel, kb, rb);
+#pragma unroll
+            for (int rb = 0; rb < RW; ++rb) l[rb] += sum[rb];
             lds_barrier();
         };
-        bool odd_seen = false;
-        auto output = [&](int rel, f32x4 (&o)[RB][NB], auto masked) __attribute__((always_inline)) {
-            const unsigned lat = (rel % X::kLatSlots) * X::kLat, prob = p_rd + (rel & 1) * X::kProb;
+        // Output of step rel, and beside it the probabilities of the scores at hand, of step rel + 1.
+        auto output = [&](int rel, int lat_slot, f32x4 (&o)[RB][NB]) __attribute__((always_inline)) {
+            const unsigned lat = lat_slot * X::kLat, prob = p_rd + (rel & 1) * X::kProb, v_here = worked_out_here(v_at);
             bf16x8 pf[RB];
+            s16x4 vf[4][2];
+            auto read = [&](int cb) __attribute__((always_inline)) {
+                const unsigned a = (v_here ^ (32 * cb)) + lat;
+                vf[cb & 3][0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + a));
+                vf[cb & 3][1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + (a ^ 16) + 4 * X::kLatRow));
+            };
+            constexpr int kAhead = NB < 3 ? NB : 3;
+            read(0);
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) pf[rb] = *reinterpret_cast<__attribute__((address_space(3))) const bf16x8*>(lds + prob + rb * 1024);
 #pragma unroll
+            for (int cb = 1; cb < kAhead; ++cb) read(cb);
+#pragma unroll
+            for (int rb = 0; rb < RW; ++rb) sum[rb] = 0.f;
+            in_this_order();
+            constexpr int kPieces = RW * KW, kEvery = NB / kPieces;
+#pragma unroll
             for (int cb = 0; cb < NB; ++cb) {
-                const unsigned a = (v_at ^ (32 * cb)) + lat;
-                s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + a));
-                s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + (a ^ 16) + 4 * X::kLatRow));
-                s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                if constexpr (decltype(masked)::value) {
-                    // A key that some row does not see may hold an infinity or NaN, and 0 times that is NaN: such values are taken out of
-                    // the product here and given to the rows that see them at the end.
-                    bool odd = false;
+                if (cb + kAhead < NB) read(cb + kAhead);
+                const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(vf[cb & 3][0], vf[cb & 3][1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if ((v[e] & 0x7F80) == 0x7F80) {
-                            odd = true;
-                            v[e] = 0;
-                        }
-                    if (__any(odd)) odd_seen = true;
-                }
-                const bf16x8 vf = __builtin_bit_cast(bf16x8, v);
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb) o[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rb], o[rb][cb], 0, 0, 0);
+                for (int rb = 0; rb < RB; ++rb) o[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[rb], o[rb][cb], 0, 0, 0);
+                if (cb % kEvery == 0) probabilities(rel + 1, (cb / kEvery) % KW, (cb / kEvery) / KW);
+                in_this_order();
             }
         };
 
         // ---- the loop ----
+        // (ring slots of step rel and of the steps behind it)
+        int lat_slot = 0, rope_slot = 0;
+        auto lat_on = [](int x, int by) { return x + by >= X::kLatSlots ? x + by - X::kLatSlots : x + by; };
+        auto rope_on = [](int x, int by) { return x + by >= X::kRopeSlots ? x + by - X::kRopeSlots : x + by; };
         if constexpr (KV8) {
             wait_vm_all();
-            convert(0);
-            if (steps > 1) convert(1);
+            convert(0, 0);
+            if (steps > 1) convert(1, 1);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the codes are read: their buffer is free)
-            if (steps > 2) issue(2);
+            if (steps > 2) issue(2, 2, 2);
             lds_barrier();
-            scores(0);
+            scores(0, 0, 0);
         } else {
             if (steps > 2) wait_vm<2 * kLoads>();
             else if (steps > 1) wait_vm<kLoads>();
             else wait_vm_all();
             lds_barrier();
-            scores(0);
+            scores(0, 0, 0);
             if (steps > 2) wait_vm<kLoads>();
             else wait_vm_all();
         }
         settle(0, true, [](auto) {});
         bool flushed = false;
-        float* const scratch = parts.o + (static_cast<size_t>(2 * split.n_wg + wl) * M + n) * R + 16 * NB * wave + 4 * g4;
-        for (int rel = 0; rel < steps;) {
-            f32x4 o[RB][NB];
+        auto scratch = [&](unsigned lane_now) {
+            return parts.o + (static_cast<size_t>(2 * split.n_wg + wl) * M + (lane_now & 15)) * R + 16 * NB * wave + 4 * (lane_now >> 4);
+        };
+        int rel = 0;
+        f32x4 o[RB][NB];
+        while (true) {
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
                 for (int cb = 0; cb < NB; ++cb) o[rb][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
-            float l_before[RW];
             bool grown = false;
-            while (!grown && rel < steps) {
-                if ((rel & 7) == 5) load_slots((rel + 3) / 8 + 1);
-                if (KV8 && rel + 2 < steps && !pure(rel + 2)) issue_direct(rel + 2);
-                if (rel + 3 < steps) issue(rel + 3);
-                if (rel + 1 < steps) {
-                    scores(rel + 1);
-#pragma unroll
-                    for (int rb = 0; rb < RW; ++rb) l_before[rb] = l[rb];
-                    probabilities(rel + 1);
-                    bool outgrown = false;
-#pragma unroll
-                    for (int rb = 0; rb < RW; ++rb) outgrown |= largest(rb) - m[rb] > kGrow;
-                    if (__any(outgrown) && lane == 0) s_flag[(rel + 1) & 1] = rel + 1;
+            while (rel < steps && !grown) {
+                if (has_hidden(rel)) {
+                    clean(lat_slot);
+                    lds_barrier();
                 }
-                if ((k0 + rel + 1) * kStep <= vis_min) output(rel, o, std::false_type{});
-                else output(rel, o, std::true_type{});
+                if ((rel & 7) == 5) load_slots((rel + 3) / 8 + 1);
+                if (KV8 && rel + 2 < steps && !pure(rel + 2)) issue_direct(rel + 2, lat_on(lat_slot, 2));
+                if (rel + 3 < steps) issue(rel + 3, KV8 ? 0 : lat_on(lat_slot, 3), rope_slot);
+                scores(rel + 1, lat_on(lat_slot, 1), rope_on(rope_slot, 1));  // (behind the last step: of whatever lies there, not used)
+                output(rel, lat_slot, o);
+                bool outgrown = false;
+#pragma unroll
+                for (int rb = 0; rb < RW; ++rb) outgrown |= sum[rb] > kMost;
+                if (__any(outgrown) && lane == 0) s_flag[(rel + 1) & 1] = rel + 1;
                 if (rel + 3 < steps && pure(rel + 3)) wait_vm<kLoads>();
                 else wait_vm_all();
-                if (KV8 && rel + 2 < steps) convert(rel + 2);
+                if (KV8 && rel + 2 < steps) convert(rel + 2, lat_on(lat_slot, 2));
                 lds_barrier();
                 ++rel;
-                grown = rel < steps && __builtin_amdgcn_readfirstlane(s_flag[rel & 1]) == rel;
-            }
-            if (grown) {
+                lat_slot = lat_on(lat_slot, 1);
+                rope_slot = rope_on(rope_slot, 1);
+                if (rel < steps) {
+                    grown = __builtin_amdgcn_readfirstlane(s_flag[rel & 1]) == rel;
+                    if (!grown)
 #pragma unroll
-                for (int rb = 0; rb < RW; ++rb) l[rb] = l_before[rb];  // (the probabilities are done again)
-                settle(rel, false, [&](auto alpha) {
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) {
-                        const float a = alpha(16 * rb + n);
-#pragma unroll
-                        for (int cb = 0; cb < NB; ++cb) {
-                            f32x4* const to = reinterpret_cast<f32x4*>(scratch + 16 * rb * R + 16 * cb);
-                            f32x4 x = o[rb][cb];
-                            if (flushed) x += *to;
-                            *to = x * a;
-                        }
-                    }
-                });
-                flushed = true;
-                continue;
-            }
-
-            // ---- the end of the tile, or of the workgroup's part of it ----
-#pragma unroll
-            for (int rb = 0; rb < RW; ++rb) {
-                const float sum = row_sum(l[rb]);
-                if (g4 == 0) s_red[kgroup * M + wrow + 16 * rb + n] = sum;
-            }
-            lds_barrier();
-            const bool head = k0 == 0, last = k1 == all_steps, whole = head && last;
-            auto row_total = [&](int row) { return KG == 2 ? s_red[row] + s_red[M + row] : s_red[row]; };
-            const int part = 2 * wl + (head ? 1 : 0);
-            if (!whole) {
-                used[head ? 1 : 0] = true;
-                if (tid == 0) parts.rec[part] = make_int4(static_cast<int>(out_row0), rows_here, (head ? kPartHead : 0) | (last ? kPartLast : 0), 1);
-                if (tid < rows_here) parts.ml[static_cast<size_t>(part) * M + tid] = make_float2(s_max[tid], row_total(tid));
-            }
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb) {
-                const int row = 16 * rb + n;
-                if (row >= rows_here) continue;
-                const float inv = whole ? 1.f / row_total(row) : 1.f;
-                const int sees = P + (row0 + row) / H + 1;
-#pragma unroll
-                for (int cb = 0; cb < NB; ++cb) {
-                    f32x4 x = o[rb][cb];
-                    if (flushed) x += *reinterpret_cast<const f32x4*>(scratch + 16 * rb * R + 16 * cb);
-                    x *= inv;
-                    const int col = 16 * (NB * wave + cb) + 4 * g4;
-                    if (odd_seen) {
-                        // (a weight is positive: an infinity stays one, two of opposite sign and NaN give NaN)
-                        for (int j = max(vis_min & ~(kStep - 1), k0 * kStep); j < min(sees, k1 * kStep); ++j) {
-                            const bool cached = j < P;
-                            if (KV8 && cached) continue;  // (the 8-bit pool holds neither)
-                            const auto* const c4 = reinterpret_cast<const unsigned short*>(row_address(j, cached ? slots[j] : 0)) + col;
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                if ((c4[i] & 0x7F80) == 0x7F80) x[i] += __uint_as_float(static_cast<unsigned>(c4[i]) << 16);
-                        }
-                    }
-                    if (whole)
-                        *reinterpret_cast<uint2*>(out + (out_row0 + row) * R + col) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
-                    else
-                        *reinterpret_cast<f32x4*>(parts.o + (static_cast<size_t>(part) * M + row) * R + col) = x;
+                        for (int rb = 0; rb < RW; ++rb) l[rb] += sum[rb];
                 }
+            }
+            if (!grown) break;
+            settle(rel, false, [&](auto alpha) {
+                const unsigned lane_now = worked_out_here(lane);
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) {
+                    const float a = alpha(16 * rb + (lane_now & 15));
+#pragma unroll
+                    for (int cb = 0; cb < NB; ++cb) {
+                        f32x4* const to = reinterpret_cast<f32x4*>(scratch(lane_now) + 16 * rb * R + 16 * cb);
+                        f32x4 x = o[rb][cb];
+                        if (flushed) x += *to;
+                        *to = x * a;
+                    }
+                }
+            });
+            flushed = true;
+        }
+
+        // ---- the end of the tile, or of the workgroup's part of it ----
+        const bool odd_seen = __builtin_amdgcn_readfirstlane(s_flag[2]) != 0;
+        const unsigned lane_now = worked_out_here(lane);
+        const int n = lane_now & 15, g4 = lane_now >> 4;
+#pragma unroll
+        for (int rb = 0; rb < RW; ++rb) {
+            const float sum = row_sum(l[rb]);
+            if (g4 == 0) s_red[kgroup * M + wrow + 16 * rb + n] = sum;
+        }
+        lds_barrier();
+        const bool head = k0 == 0, last = k1 == all_steps, whole = head && last;
+        auto row_total = [&](int row) { return KG == 2 ? s_red[row] + s_red[M + row] : s_red[row]; };
+        const int part = 2 * wl + (head ? 1 : 0);
+        if (!whole) {
+            used[head ? 1 : 0] = true;
+            if (tid == 0) parts.rec[part] = make_int4(static_cast<int>(out_row0), rows_here, (head ? kPartHead : 0) | (last ? kPartLast : 0), 1);
+            if (tid < rows_here) parts.ml[static_cast<size_t>(part) * M + tid] = make_float2(s_max[tid], row_total(tid));
+        }
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            const int row = 16 * rb + n;
+            if (row >= rows_here) continue;
+            const float inv = whole ? 1.f / row_total(row) : 1.f;
+            const int sees = P + (row0 + row) / H + 1;
+#pragma unroll
+            for (int cb = 0; cb < NB; ++cb) {
+                f32x4 x = o[rb][cb];
+                if (flushed) x += *reinterpret_cast<const f32x4*>(scratch(lane_now) + 16 * rb * R + 16 * cb);
+                x *= inv;
+                const int col = 16 * (NB * wave + cb) + 4 * g4;
+                if (odd_seen) {
+                    // (a weight is positive: an infinity stays one, two of opposite sign and NaN give NaN)
+                    for (int j = max(vis_min & ~(kStep - 1), k0 * kStep); j < min(sees, k1 * kStep); ++j) {
+                        const bool cached = j < P;
+                        if (KV8 && cached) continue;  // (the 8-bit pool holds neither)
+                        const auto* const c4 = reinterpret_cast<const unsigned short*>(row_address(j, cached ? slots[j] : 0)) + col;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if ((c4[i] & 0x7F80) == 0x7F80) x[i] += __uint_as_float(static_cast<unsigned>(c4[i]) << 16);
+                    }
+                }
+                if (whole)
+                    *reinterpret_cast<uint2*>(out + (out_row0 + row) * R + col) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+                else
+                    *reinterpret_cast<f32x4*>(parts.o + (static_cast<size_t>(part) * M + row) * R + col) = x;
             }
         }
         lds_barrier();
