@@ -38,6 +38,16 @@ namespace pa {
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
+// The products of the scores, with their results in vector registers: left to the compiler they take accumulation registers, of which the output needs all
+// 256, and are copied.  What reads the results waits for them first (products_done).
+__device__ __forceinline__ void mfma_first(f32x4& d, bf16x8 a, bf16x8 b) {
+    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=&v"(d) : "v"(a), "v"(b));
+}
+__device__ __forceinline__ void mfma_next(f32x4& d, bf16x8 a, bf16x8 b) {
+    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(d) : "v"(a), "v"(b));
+}
+__device__ __forceinline__ void products_done() { asm volatile("s_nop 15\n\ts_nop 3" ::: "memory"); }
+
 constexpr int kStep = 32;       // keys of a step
 constexpr float kMost = 1099511627776.f;  // 2^40
 
@@ -55,7 +65,7 @@ template <int R, int M, bool KV8>
 struct LatentShape {
     static constexpr int kAhead = M == 128 ? 2 : 3;  // steps that loads are ahead of the step whose output is computed
     static constexpr int kLatRow = 2 * R, kLat = kStep * kLatRow;  // bytes of a latent row and of a step's
-    static constexpr int kLatSlots = KV8 ? 3 : kAhead + 1, kRopeSlots = kAhead, kRopeStep = kStep * 2 * kRope;
+    static constexpr int kLatSlots = KV8 ? 3 : kAhead + 1, kRopeSlots = kAhead + 1, kRopeStep = kStep * 2 * kRope;
     static constexpr int kCodes = KV8 ? kStep * R : 0, kCodeSlots = kAhead - 1;
     static constexpr int kProb = M * kStep * 2;
     // slices of 32 values of Q that lie in LDS and not in registers
@@ -152,46 +162,53 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
                 load_to_lds_4(slots + min(j, P - 1), lds0 + X::kSlotsAt + wave * 512 + (blk & 1) * 256);
             }
         };
-        auto issue = [&](int rel, int lat_slot, int rope_slot) __attribute__((always_inline)) {
+        // The loads of a step, in kIssue pieces, so that they can stand between matrix instructions: what they need, then one or two at a time.  (Steps behind
+        // the last are loaded too, as rows of zeros: every interval has the same loads.)
+        uint64_t row_at = 0, rope_at = 0;
+        int slot_a = 0, slot_b = 0;
+        constexpr int kRowLoads = KV8 ? 8 * R / 1024 : 8 / RPL, kIssue = 3 + kRowLoads;
+        auto issue_piece = [&](int piece, int rel, int lat_slot, int rope_slot) __attribute__((always_inline)) {
+            const int lane = static_cast<int>(worked_out_here(tid)) & 63;
             const int j0 = (k0 + rel) * kStep + 8 * wave;
             const int* const sl = s_slots + ((rel >> 3) & 1) * 64 + (rel & 7) * 8;
-            [[maybe_unused]] const unsigned lat = lds0 + lat_slot * X::kLat + 8 * wave * X::kLatRow;
-            const unsigned rope = lds0 + X::kRopeAt + rope_slot * X::kRopeStep + 8 * wave * 2 * kRope;
-            if constexpr (!KV8 && RPL == 1) {
-                const uint64_t a = row_address(j0 + (lane & 7), sl[lane & 7]);
-                const unsigned lo = static_cast<unsigned>(a), hi = static_cast<unsigned>(a >> 32);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    // (readlane gives a signed word: it must not be extended by its sign)
-                    const uint64_t base = static_cast<unsigned>(__builtin_amdgcn_readlane(lo, i)) | static_cast<uint64_t>(static_cast<unsigned>(__builtin_amdgcn_readlane(hi, i))) << 32;
-                    load_to_lds_16(reinterpret_cast<const void*>(base), 16u * (lane ^ swz((8 * wave + i) & 15)), lat + i * X::kLatRow);
+            if (piece == 0) {
+                slot_a = sl[lane & 7];
+                slot_b = sl[lane >> 3];
+            } else if (piece == 1) {
+                row_at = row_address(j0 + (lane & 7), slot_a);
+                const int row = lane >> 3, j = j0 + row;
+                rope_at = row_address(j, slot_b) + ((KV8 && j < P ? R : 2 * R) + 16 * ((lane & 7) ^ swz_rope((8 * wave + row) & 15)));
+            } else if (piece == 2) {
+                load_to_lds_16(reinterpret_cast<const void*>(rope_at), lds0 + X::kRopeAt + rope_slot * X::kRopeStep + 8 * wave * 2 * kRope);
+                if constexpr (KV8) {
+                    const unsigned char* const exps = pool + static_cast<uint64_t>(b.num_slots) * PROW;
+                    if (lane < 8 && j0 + lane < P)
+                        load_to_lds_1(exps + min(static_cast<unsigned>(max(slot_a, 0)), static_cast<unsigned>(b.num_slots - 1)),
+                                      lds0 + X::kExpAt + wave * 64 + (rel & 1) * 32);
                 }
-            } else if constexpr (!KV8) {
-#pragma unroll
-                for (int i = 0; i < 8 / RPL; ++i) {
-                    const int row = i * RPL + lane / (64 / RPL);
-                    load_to_lds_16(reinterpret_cast<const unsigned char*>(row_address(j0 + row, sl[row])) + 16 * ((lane & (64 / RPL - 1)) ^ swz((8 * wave + row) & 15)),
-                                   lat + i * 1024);
-                }
-            }
-            if constexpr (KV8) {
-                const unsigned char* const exps = pool + static_cast<uint64_t>(b.num_slots) * PROW;
-#pragma unroll
-                for (int i = 0; i < 8 * R / 1024; ++i) {
+            } else {
+                const int i = piece - 3;
+                if constexpr (KV8) {
                     const int row = i * (1024 / R) + lane / (R / 16);
                     if (j0 + row < P)
                         load_to_lds_16(reinterpret_cast<const unsigned char*>(row_address(j0 + row, sl[row])) + 16 * (lane % (R / 16)),
                                        lds0 + X::kCodesAt + (rel & (X::kCodeSlots - 1)) * X::kCodes + 8 * wave * R + i * 1024);
+                } else if constexpr (RPL == 1) {
+                    const unsigned lo = static_cast<unsigned>(row_at), hi = static_cast<unsigned>(row_at >> 32);
+                    // (readlane gives a signed word: it must not be extended by its sign)
+                    const uint64_t base = static_cast<unsigned>(__builtin_amdgcn_readlane(lo, i)) | static_cast<uint64_t>(static_cast<unsigned>(__builtin_amdgcn_readlane(hi, i))) << 32;
+                    load_to_lds_16(reinterpret_cast<const void*>(base), 16u * (lane ^ swz((8 * wave + i) & 15)), lds0 + lat_slot * X::kLat + (8 * wave + i) * X::kLatRow);
+                } else {
+                    const int row = i * RPL + lane / (64 / RPL);
+                    load_to_lds_16(reinterpret_cast<const unsigned char*>(row_address(j0 + row, sl[row])) + 16 * ((lane & (64 / RPL - 1)) ^ swz((8 * wave + row) & 15)),
+                                   lds0 + lat_slot * X::kLat + 8 * wave * X::kLatRow + i * 1024);
                 }
-                if (lane < 8 && j0 + lane < P)
-                    load_to_lds_1(exps + min(static_cast<unsigned>(max(sl[lane], 0)), static_cast<unsigned>(b.num_slots - 1)),
-                                  lds0 + X::kExpAt + wave * 64 + (rel & 1) * 32);
             }
-            const int row = lane >> 3, j = j0 + row;
-            const uint64_t a = row_address(j, sl[row]);
-            load_to_lds_16(reinterpret_cast<const unsigned char*>(a) + (KV8 && j < P ? R : 2 * R) + 16 * ((lane & 7) ^ swz_rope((8 * wave + row) & 15)), rope);
         };
-
+        auto issue = [&](int rel, int lat_slot, int rope_slot) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < kIssue; ++i) issue_piece(i, rel, lat_slot, rope_slot);
+        };
         // 8-bit pool.  All rows of a step are in the pool: its loads are kLoads, no row goes to its place in LDS directly.
         auto pure = [&](int rel) { return !KV8 || (k0 + rel + 1) * kStep <= P; };
         // rows that are bf16 in memory (extend tokens, and what stands for keys behind the last), to their place
@@ -227,12 +244,10 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
         // ---- the wave's rows of Q ----
         constexpr int KQ = KS + KSR - X::kQLds;  // slices in registers
         bf16x8 q[RW][KQ];
-        int vis[RW];
         load_slots(0);
 #pragma unroll
         for (int rb = 0; rb < RW; ++rb) {
             const int row = min(wrow + 16 * rb + n, rows_here - 1);  // (rows behind the last repeat it)
-            vis[rb] = P + (row0 + row) / H + 1;
             const uint4* const src = reinterpret_cast<const uint4*>(q_ext + (out_row0 + row) * L);
 #pragma unroll
             for (int s = 0; s < KQ; ++s) q[rb][s] = __builtin_bit_cast(bf16x8, src[4 * s + g4]);
@@ -259,7 +274,7 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
         // its scores are done, the wave that loaded a row takes such values out of it; the end of the tile gives them to the rows that see them.
         auto has_hidden = [&](int rel) { return vis_min < key_end && (k0 + rel + 1) * kStep > vis_min; };
         auto clean = [&](int lat_slot) {
-            const unsigned at_row = lat_slot * X::kLat + 8 * wave * X::kLatRow + 16 * lane;
+            const unsigned at_row = lat_slot * X::kLat + 8 * wave * X::kLatRow + 16 * worked_out_here(lane);
 #pragma unroll
             for (int i = 0; i < 8 / RPL; ++i) {
                 auto* const c8 = reinterpret_cast<__attribute__((address_space(3))) s16x8*>(lds + at_row + 1024 * i);
@@ -278,9 +293,11 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
             }
         };
         f32x4 sc[KW][RW];
-        // Scores of a step; fragments are read kAhead ahead.
-        auto scores = [&](int rel, int lat_slot, int rope_slot) __attribute__((always_inline)) {
+        // Scores of a step; fragments are read kAhead ahead.  Between the products, the loads of step load_rel.
+        auto scores = [&](int rel, int lat_slot, int rope_slot, auto with, int load_rel, int load_lat, int load_rope) __attribute__((always_inline)) {
+            constexpr bool loads = decltype(with)::value;
             constexpr int kFrags = KW * (KS + KSR), kAhead = 4;
+            static_assert(kIssue <= kFrags, "a product for each of them");
             const unsigned lat = lat_slot * X::kLat, rope = rope_slot * X::kRopeStep;
             u32x4 kf[kAhead + 1];
             u32x4 qf[2][RW];  // (of the slices of Q in LDS, one ahead)
@@ -303,18 +320,29 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
                 if (kb == 0 && s + 1 >= KQ && s + 1 < KS + KSR) read_q(s + 1);
 #pragma unroll
                 for (int rb = 0; rb < RW; ++rb)
-                    sc[kb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[f % (kAhead + 1)]), s < KQ ? q[rb][s < KQ ? s : 0] : __builtin_bit_cast(bf16x8, qf[s & 1][rb]), s == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sc[kb][rb], 0, 0, 0);
+                    if (s == 0) mfma_first(sc[kb][rb], __builtin_bit_cast(bf16x8, kf[f % (kAhead + 1)]), q[rb][0]);
+                    else mfma_next(sc[kb][rb], __builtin_bit_cast(bf16x8, kf[f % (kAhead + 1)]), s < KQ ? q[rb][s < KQ ? s : 0] : __builtin_bit_cast(bf16x8, qf[s & 1][rb]));
+                if constexpr (loads) {
+                    // (as early as can be: spread over all of the products, a step of 128 rows took a tenth longer)
+                    if (f < kIssue) issue_piece(f, load_rel, load_lat, load_rope);
+                }
                 in_this_order();
             }
+            products_done();
+            in_this_order();
             const int j0 = (k0 + rel) * kStep;
             if (j0 + kStep > vis_min) {
+                const int lane_now = static_cast<int>(worked_out_here(lane));
 #pragma unroll
-                for (int kb = 0; kb < KW; ++kb)
+                for (int rb = 0; rb < RW; ++rb) {
+                    const int row = min(wrow + 16 * rb + (lane_now & 15), rows_here - 1);
+                    const int sees = P + (row0 + row) / H + 1 - j0 - wkey - 4 * (lane_now >> 4);
 #pragma unroll
-                    for (int rb = 0; rb < RW; ++rb)
+                    for (int kb = 0; kb < KW; ++kb)
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            if (j0 + wkey + 16 * kb + 4 * g4 + i >= vis[rb]) sc[kb][rb][i] = -INFINITY;
+                            if (16 * kb + i >= sees) sc[kb][rb][i] = -INFINITY;
+                }
             }
         };
         // a piece of the probabilities of the scores against the maxima as they stand, into buffer rel % 2; their sums
@@ -346,6 +374,7 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
                 if (g4 == 0) s_red[kgroup * M + wrow + 16 * rb + n] = mx;
             }
             lds_barrier();
+            if (tid < 2) s_flag[tid] = -1;  // (all waves have looked)
             auto new_max = [&](int row) {
                 float x = s_red[row];
                 if (KG == 2) x = fmaxf(x, s_red[M + row]);
@@ -367,37 +396,47 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
             for (int rb = 0; rb < RW; ++rb)
 #pragma unroll
                 for (int kb = 0; kb < KW; ++kb) probabilities(rel, kb, rb);
-#pragma unroll
-            for (int rb = 0; rb < RW; ++rb) l[rb] += sum[rb];
             lds_barrier();
         };
         // Output of step rel, and beside it the probabilities of the scores at hand, of step rel + 1.
-        auto output = [&](int rel, int lat_slot, f32x4 (&o)[RB][NB]) __attribute__((always_inline)) {
+        bf16x8 pf[RB];
+        s16x4 vf[4][2];
+        constexpr int kVAhead = NB < 3 ? NB : 3;
+        auto read_v = [&](int cb, unsigned v_here, unsigned lat) __attribute__((always_inline)) {
+            const unsigned a = (v_here ^ (32 * cb)) + lat;
+            vf[cb & 3][0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + a));
+            vf[cb & 3][1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + (a ^ 48) + 4 * X::kLatRow));
+        };
+        auto output_reads = [&](int rel, int lat_slot) __attribute__((always_inline)) {
             const unsigned lat = lat_slot * X::kLat, prob = p_rd + (rel & 1) * X::kProb, v_here = worked_out_here(v_at);
-            bf16x8 pf[RB];
-            s16x4 vf[4][2];
-            auto read = [&](int cb) __attribute__((always_inline)) {
-                const unsigned a = (v_here ^ (32 * cb)) + lat;
-                vf[cb & 3][0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + a));
-                vf[cb & 3][1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + (a ^ 48) + 4 * X::kLatRow));
-            };
-            constexpr int kAhead = NB < 3 ? NB : 3;
-            read(0);
+            read_v(0, v_here, lat);
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) pf[rb] = *reinterpret_cast<__attribute__((address_space(3))) const bf16x8*>(lds + prob + rb * 1024);
 #pragma unroll
-            for (int cb = 1; cb < kAhead; ++cb) read(cb);
+            for (int cb = 1; cb < kVAhead; ++cb) read_v(cb, v_here, lat);
+            in_this_order();
+        };
+        auto output = [&](int rel, int lat_slot, f32x4 (&o)[RB][NB]) __attribute__((always_inline)) {
+            const unsigned lat = lat_slot * X::kLat, v_here = worked_out_here(v_at);
 #pragma unroll
             for (int rb = 0; rb < RW; ++rb) sum[rb] = 0.f;
-            in_this_order();
-            constexpr int kPieces = RW * KW, kEvery = NB / kPieces;
+            constexpr int kPieces = RW * KW, kEvery = NB / kPieces, kInVector = KV8 ? 1 : 2;
 #pragma unroll
             for (int cb = 0; cb < NB; ++cb) {
-                if (cb + kAhead < NB) read(cb + kAhead);
+                if (cb + kVAhead < NB) read_v(cb + kVAhead, v_here, lat);
                 const bf16x8 v = __builtin_bit_cast(bf16x8, __builtin_shufflevector(vf[cb & 3][0], vf[cb & 3][1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-                for (int rb = 0; rb < RB; ++rb) o[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[rb], o[rb][cb], 0, 0, 0);
+                for (int rb = 0; rb < RB; ++rb) {
+                    // (128 rows and 512 columns are all accumulation registers there are; what else the compiler wants some for would cost a block of the
+                    // output a place in memory, and a wait for all loads each time: a few blocks have vector registers)
+                    if (RB * NB == 64 && rb == RB - 1 && cb >= NB - kInVector) mfma_next(o[rb][cb], v, pf[rb]);
+                    else o[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[rb], o[rb][cb], 0, 0, 0);
+                }
                 if (cb % kEvery == 0) probabilities(rel + 1, (cb / kEvery) % KW, (cb / kEvery) / KW);
+                in_this_order();
+            }
+            if constexpr (RB * NB == 64) {
+                products_done();
                 in_this_order();
             }
         };
@@ -419,7 +458,7 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
                 if (!pure(1)) issue_direct(1, 1);
             }
             lds_barrier();
-            scores(0, 0, 0);
+            scores(0, 0, 0, std::false_type{}, 0, 0, 0);
             if (X::kAhead == 2 && steps > 1) {
                 wait_vm_all();
                 convert(1, 1);
@@ -429,7 +468,7 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
             else if (steps > 1) wait_vm<kLoads>();
             else wait_vm_all();
             lds_barrier();
-            scores(0, 0, 0);
+            scores(0, 0, 0, std::false_type{}, 0, 0, 0);
             if (X::kAhead == 3 && steps > 2) wait_vm<kLoads>();
             else wait_vm_all();
         }
@@ -438,7 +477,7 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
         auto scratch = [&](unsigned lane_now) {
             return parts.o + (static_cast<size_t>(2 * split.n_wg + wl) * M + (lane_now & 15)) * R + 16 * NB * wave + 4 * (lane_now >> 4);
         };
-        int rel = 0;
+        int rel = 0;  // (the sums of its probabilities are taken up when these are used)
         f32x4 o[RB][NB];
         while (true) {
 #pragma unroll
@@ -446,35 +485,45 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
 #pragma unroll
                 for (int cb = 0; cb < NB; ++cb) o[rb][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
             bool grown = false;
-            while (rel < steps && !grown) {
+            while (true) {
+                const int flag = s_flag[rel & 1];
+                if ((rel & 7) == 8 - X::kAhead) load_slots((rel + X::kAhead) / 8 + 1);
+                if (KV8 && rel + 2 < steps && !pure(rel + 2)) issue_direct(rel + 2, lat_on(lat_slot, 2));
+                // (behind the last step: of whatever lies there, not used)
+                scores(rel + 1, lat_on(lat_slot, 1), rope_on(rope_slot, 1), std::true_type{}, rel + X::kAhead, KV8 ? 0 : lat_on(lat_slot, X::kAhead), rope_on(rope_slot, X::kAhead));
+                if (__builtin_amdgcn_readfirstlane(flag) == rel) {
+                    grown = true;
+                    break;
+                }
+#pragma unroll
+                for (int rb = 0; rb < RW; ++rb) l[rb] += sum[rb];
                 if (has_hidden(rel)) {
                     clean(lat_slot);
                     lds_barrier();
                 }
-                if ((rel & 7) == 8 - X::kAhead) load_slots((rel + X::kAhead) / 8 + 1);
-                if (KV8 && rel + 2 < steps && !pure(rel + 2)) issue_direct(rel + 2, lat_on(lat_slot, 2));
-                if (rel + X::kAhead < steps) issue(rel + X::kAhead, KV8 ? 0 : lat_on(lat_slot, X::kAhead), rope_slot);
-                scores(rel + 1, lat_on(lat_slot, 1), rope_on(rope_slot, 1));  // (behind the last step: of whatever lies there, not used)
+                output_reads(rel, lat_slot);
                 output(rel, lat_slot, o);
                 bool outgrown = false;
 #pragma unroll
                 for (int rb = 0; rb < RW; ++rb) outgrown |= sum[rb] > kMost;
                 if (__any(outgrown) && lane == 0) s_flag[(rel + 1) & 1] = rel + 1;
-                if (X::kAhead == 3 && rel + 3 < steps && pure(rel + 3)) wait_vm<kLoads>();
+                if (X::kAhead == 3 && pure(rel + 3)) wait_vm<kLoads>();
                 else wait_vm_all();
                 if (KV8 && rel + 2 < steps) convert(rel + 2, lat_on(lat_slot, 2));
                 lds_barrier();
                 ++rel;
                 lat_slot = lat_on(lat_slot, 1);
                 rope_slot = rope_on(rope_slot, 1);
-                if (rel < steps) {
-                    grown = __builtin_amdgcn_readfirstlane(s_flag[rel & 1]) == rel;
-                    if (!grown)
-#pragma unroll
-                        for (int rb = 0; rb < RW; ++rb) l[rb] += sum[rb];
-                }
+                if (rel >= steps) break;
             }
-            if (!grown) break;
+            products_done();
+            if (!grown) {
+                wait_vm_all();  // (nothing is on its way to LDS any more)
+                break;
+            }
+            // (the scores of this step once more, and what is on its way to LDS has landed before it is asked for again)
+            wait_vm_all();
+            scores(rel, lat_slot, rope_slot, std::false_type{}, 0, 0, 0);
             settle(rel, false, [&](auto alpha) {
                 const unsigned lane_now = worked_out_here(lane);
 #pragma unroll
