@@ -4,7 +4,7 @@
 // costs 4 N R operations per row and head, as much as 171 rows of q save.  So it is done once for each row the batch sees, however many
 // requests share it:
 //   mark     every slot of the lists takes a number, the first time it is met (a word per slot of the pool, cleared before)
-//   collect  the rows with numbers, decoded, and the extend rows before them, behind one another: A [rows, R + kRope]; the lists become row numbers
+//   collect  the rows with numbers, decoded, and the extend rows before them, behind one another: A [rows, R], A_r [rows, kRope]; the lists become row numbers
 //   expand   K [head, row, N] = A W_k^T, V likewise, on the matrix cores; fp16 out of fp32 sums
 //   attend   softmax(Q K^T + Q_r A_r^T) V
 // Expanded keys and values lie in the workspace for as many heads at a time as fit kExpandedBytes.
@@ -31,6 +31,13 @@ typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
+template <typename T>
+using Global = __attribute__((address_space(1))) T;  // (an address that was a number is of no known memory otherwise)
+
+// max(m, |a|, |b|) in one instruction, NaN aside.  The operands are results of matrix instructions that are done (products_done).
+__device__ __forceinline__ void larger_of(float& m, float a, float b) { asm volatile("v_max3_f32 %0, |%1|, |%2|, %0" : "+v"(m) : "v"(a), "v"(b)); }
+__device__ __forceinline__ void products_done() { asm volatile("s_nop 15\n\ts_nop 3" ::: "memory"); }
+
 constexpr size_t kExpandedBytes = size_t{4} << 30;
 constexpr int kExpandWorkgroups = 256;  // one on a compute unit
 constexpr int kExpWorkgroups = 512;     // two
@@ -50,7 +57,7 @@ struct ExpandArgs {
     int32_t *map;      // [num_slots]
     int32_t *list;     // [cached_cap]
     int32_t *row_of;   // [B][max_keys] rows of A of a request's keys, cached and new
-    __hip_bfloat16* a; // [rows_cap][R + kRope]
+    uint4 *a, *rope;   // latent parts [rows_cap / 16][R / 32][64 lanes], as fragments (see collect); rotary parts [rows_cap][8]
     signed char *k_exp, *v_exp;  // [heads at once][rows_cap / 64]
     unsigned short *k, *v;       // [heads at once][rows_cap][N] fp16
     int64_t cached_cap, rows_cap;
@@ -89,29 +96,40 @@ __global__ __launch_bounds__(256) void latent_mark_kernel(LatentBatch b, ExpandA
     }
 }
 
-// Waves take rows of A and, when these are done, 64 keys of a request at a time.
+// Waves take 16 rows of A at a time and, when these are done, 64 keys of a request.
+// A lies in memory as the fragments that the matrix cores take: of 16 rows and 32 columns, 16 bytes (row lane % 16, columns 8 (lane / 16) on) of every lane
+// behind one another, so that the expansion reads 1 KB of consecutive memory an instruction, straight into registers.
 template <int R, bool KV8>
 __global__ __launch_bounds__(256) void latent_collect_kernel(LatentBatch b, ExpandArgs x) {
-    constexpr int L = R + kRope, PROW = KV8 ? R + 2 * kRope : 2 * L, LPR = R / 8;  // 16-byte pieces of the latent part of a row of A
-    const int lane = threadIdx.x & 63, waves = gridDim.x * 4, wave = blockIdx.x * 4 + (threadIdx.x >> 6);
+    constexpr int L = R + kRope, PROW = KV8 ? R + 2 * kRope : 2 * L;
+    const int lane = threadIdx.x & 63, n = lane & 15, g4 = lane >> 4, waves = gridDim.x * 4, wave = blockIdx.x * 4 + (threadIdx.x >> 6);
     const int64_t rows = b.T + min(static_cast<int64_t>(x.hdr[8]), x.cached_cap);
     const unsigned char* const pool = static_cast<const unsigned char*>(b.pool);
-    for (int64_t row = wave; row < rows; row += waves) {
-        uint4* const to = reinterpret_cast<uint4*>(x.a + row * L);
+    for (int64_t block = wave; block < (rows + 15) / 16; block += waves) {
+        const int64_t row = min(16 * block + n, rows - 1);  // (rows behind the last repeat it)
+        uint4* const to = x.a + block * (2 * R) + lane;
+        const uint4* rope;
         if (row < b.T || !KV8) {
             const uint4* const from = row < b.T ? reinterpret_cast<const uint4*>(static_cast<const __hip_bfloat16*>(b.c_ext) + row * L)
                                                 : reinterpret_cast<const uint4*>(pool + static_cast<int64_t>(x.list[row - b.T]) * PROW);
-            for (int c = lane; c < L / 8; c += 64) to[c] = from[c];
-        } else if constexpr (KV8) {
+#pragma unroll 8
+            for (int s = 0; s < R / 32; ++s) to[64 * s] = from[4 * s + g4];
+            rope = from + R / 8;
+        } else {
             const int64_t slot = x.list[row - b.T];
-            const unsigned char* const from = pool + slot * PROW;
+            const uint2* const from = reinterpret_cast<const uint2*>(pool + slot * PROW);
             const float two_k = fp8_scale(reinterpret_cast<const signed char*>(pool + b.num_slots * PROW)[slot]);
-            if (lane < LPR) {
-                const uint2 codes = reinterpret_cast<const uint2*>(from)[lane];
+#pragma unroll 8
+            for (int s = 0; s < R / 32; ++s) {
+                const uint2 codes = from[4 * s + g4];
                 const uint2 p = fp8_decode4(codes.x, two_k), q = fp8_decode4(codes.y, two_k);
-                to[lane] = make_uint4(p.x, p.y, q.x, q.y);
+                to[64 * s] = make_uint4(p.x, p.y, q.x, q.y);
             }
-            if (lane < kRope / 8) to[LPR + lane] = reinterpret_cast<const uint4*>(from + R)[lane];
+            rope = reinterpret_cast<const uint4*>(from + R / 8);
+        }
+        if (16 * block + n < rows) {
+            x.rope[row * 8 + g4] = rope[g4];
+            x.rope[row * 8 + 4 + g4] = rope[4 + g4];
         }
     }
     const int chunks = (x.max_keys + 63) / 64;
@@ -128,136 +146,150 @@ __global__ __launch_bounds__(256) void latent_collect_kernel(LatentBatch b, Expa
     }
 }
 
-// K and V of the heads h0 .. h0 + heads - 1.  The unit of work is 256 rows by 128 of a head's 2 N columns (its keys, then its values), the units of one set
-// of columns behind one another; a workgroup takes an equal share of them.  The 128 columns of W stay in LDS, 128 KB at R = 512; a wave
-// multiplies 64 rows, straight from memory, so that a fragment of W is read from LDS for four products and nothing is waited for but the first load of W.
+// K and V of the heads h0 .. h0 + heads - 1, as one product of A with sets of 128 of a head's 2 N columns (its keys', then its values').  A wave multiplies
+// 64 rows with the 128 columns: those of W stay in LDS, 128 KB at R = 512, where a fragment is read for four products; A's fragments
+// come straight from memory.  An XCD has an eighth of the rows, so that they stay in its L2, and its 32 workgroups equal shares of the (set, 64 rows)
+// there, set by set; the eight waves of a workgroup go through a set's part of the share one beside the other,
+// without waiting for each other, so that of the two on a SIMD one multiplies while the other packs and stores.
 template <int R, int N>
-__global__ __launch_bounds__(256, 1) void latent_expand_kernel(ExpandArgs x, const __hip_bfloat16* __restrict__ w_k, const __hip_bfloat16* __restrict__ w_v,
+__global__ __launch_bounds__(512, 1) void latent_expand_kernel(ExpandArgs x, const __hip_bfloat16* __restrict__ w_k, const __hip_bfloat16* __restrict__ w_v,
                                                                int64_t T, int h0, int heads) {
-    constexpr int L = R + kRope, KS = R / 32, kSets = 2 * N / 128;  // sets of 128 columns per head
+    constexpr int KS = R / 32, kSets = 2 * N / 128;  // slices of 32 values; sets of 128 columns per head
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     auto* const lds = (__attribute__((address_space(3))) unsigned char*)smem;
     const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_address(smem));
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g4 = lane >> 4;
     const int64_t rows = T + min(static_cast<int64_t>(x.hdr[8]), x.cached_cap);
-    const int64_t blocks = (rows + 255) / 256, units = blocks * heads * kSets;
-    const int wg = blockIdx.x;
-    int64_t unit = units * wg / gridDim.x;
-    const int64_t end = units * (wg + 1) / gridDim.x;
-    // A unit's rows of A are asked for kAhead slices of 32 values ahead, the first of the next unit's beside the last products of this one's.
-    constexpr int kAhead = 4;
-    auto row_of_unit = [&](int64_t u) { return (u % blocks) * 256 + 64 * wave; };
-    const uint4* from[4];
-    auto point_at = [&](int64_t u) {
+    const int blocks = static_cast<int>((rows + 63) / 64), last16 = static_cast<int>((rows + 15) / 16) - 1;
+    // (workgroups go to the XCDs in turn)
+    constexpr int kXcds = 8, kPerXcd = kExpandWorkgroups / kXcds;
+    const int xcd = blockIdx.x % kXcds, mine = blockIdx.x / kXcds;
+    const int first = static_cast<int>(static_cast<int64_t>(blocks) * xcd / kXcds), here = static_cast<int>(static_cast<int64_t>(blocks) * (xcd + 1) / kXcds) - first;
+    const int64_t units = static_cast<int64_t>(here) * heads * kSets;
+    int64_t unit = units * mine / kPerXcd;
+    const int64_t end = units * (mine + 1) / kPerXcd;
+    // A block's fragments are asked for kAhead slices ahead, the first of the next block's beside the last products of this one's.
+    constexpr int kAhead = 2;
+    uint64_t from[4];
+    auto point_at = [&](int block) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) from[r] = reinterpret_cast<const uint4*>(x.a + min(row_of_unit(u) + 16 * r + n, rows - 1) * L) + 2 * g4;
+        for (int r = 0; r < 4; ++r)  // (see collect)
+            from[r] = reinterpret_cast<uint64_t>(x.a) + static_cast<uint64_t>(static_cast<unsigned>(__builtin_amdgcn_readfirstlane(min(4 * block + r, last16)))) * (32 * R);
     };
-    // (a lane takes 32 bytes behind one another for two slices, so that a line of memory is used at once; the order of a sum's terms is free)
     u32x4 af[kAhead][4];
-    auto fetch_two = [&](int s) __attribute__((always_inline)) {
+    auto fetch = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int t = 0; t < 2; ++t) af[(s + t) % kAhead][r] = __builtin_bit_cast(u32x4, from[r][4 * s + t]);
+            af[s % kAhead][r] = *reinterpret_cast<Global<const u32x4>*>(reinterpret_cast<Global<const unsigned char>*>(from[r] + 1024 * s) + 16u * static_cast<unsigned>(lane));
     };
-    unsigned w_at[4];  // LDS address of a fragment of W, by its slice mod 4
+    // Fragments 2 p and 2 p + 1 of W have the columns 32 p + 8 (n / 4) + n % 4, and 4 more, so that a lane's sums of both are 8 columns behind one another, and
+    // are stored in 16 bytes.  The pieces of 16 bytes of a column are XORed by n.
+    unsigned w_at[4];  // LDS address of a fragment, by its slice mod 4
 #pragma unroll
-    for (int s = 0; s < 4; ++s) w_at[s] = n * 2 * R + 16 * ((8 * (s >> 1) + 2 * g4 + (s & 1)) ^ n);
-    int have = -1;
-    if (unit < end) {
-        point_at(unit);
-#pragma unroll
-        for (int s = 0; s < kAhead; s += 2) fetch_two(s);
-    }
-    for (; unit < end; ++unit) {
-        const int set = static_cast<int>(unit / blocks), h = set / kSets;
-        const int64_t row0 = row_of_unit(unit);
-        if (set != have) {
-            have = set;
-            lds_barrier();  // (nobody reads the old columns any more)
-            constexpr int kRowsPerLoad = 512 / R;
-            for (int i = wave; i < 128 / kRowsPerLoad; i += 4) {
-                const int row = i * kRowsPerLoad + lane / (64 / kRowsPerLoad);
-                const int col = (set % kSets) * 128 + row;  // among the head's 2 N
-                const __hip_bfloat16* const w = (col < N ? w_k : w_v) + (static_cast<int64_t>(h0 + h) * N + (col < N ? col : col - N)) * R;
-                load_to_lds_16(w + 8 * ((lane & (64 / kRowsPerLoad - 1)) ^ (row & 15)), lds0 + i * 1024);
-            }
-            wait_vm_all();
-            lds_barrier();
+    for (int s = 0; s < 4; ++s) w_at[s] = (8 * (n >> 2) + (n & 3)) * 2 * R + 16 * ((4 * s + g4) ^ n);
+    while (unit < end) {
+        const int set = static_cast<int>(unit / here), h = set / kSets;
+        const int from_block = static_cast<int>(unit - static_cast<int64_t>(set) * here), blocks_here = static_cast<int>(min(end - unit, static_cast<int64_t>(here - from_block)));
+        unit += blocks_here;
+        lds_barrier();  // (nobody reads the old columns any more)
+        constexpr int kRowsPerLoad = 512 / R;
+        for (int i = wave; i < 128 / kRowsPerLoad; i += 8) {
+            const int row = i * kRowsPerLoad + lane / (64 / kRowsPerLoad);
+            const int col = (set % kSets) * 128 + row;  // among the head's 2 N
+            const __hip_bfloat16* const w = (col < N ? w_k : w_v) + (static_cast<int64_t>(h0 + h) * N + (col < N ? col : col - N)) * R;
+            load_to_lds_16(w + 8 * ((lane & (64 / kRowsPerLoad - 1)) ^ ((row & 3) | (row >> 1 & 12))), lds0 + i * 1024);
         }
-        f32x4 acc[8][4];
+        int at = wave;
+        if (at < blocks_here) {
+            point_at(first + from_block + at);
 #pragma unroll
-        for (int c = 0; c < 8; ++c)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc[c][r] = f32x4{0.f, 0.f, 0.f, 0.f};
-        constexpr int kWAhead = 3;
-        u32x4 wf[kWAhead + 1];
-        auto read = [&](int f) __attribute__((always_inline)) {
-            const int s = f >> 3, c = f & 7;
-            wf[f % (kWAhead + 1)] = *reinterpret_cast<__attribute__((address_space(3))) const u32x4*>(lds + w_at[s & 3] + c * 16 * 2 * R + (s >> 2) * 256);
-        };
-#pragma unroll
-        for (int f = 0; f < kWAhead; ++f) read(f);
-        in_this_order();
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            if (s + kAhead == KS) point_at(min(unit + 1, end - 1));  // (KS, kAhead: even)
-#pragma unroll
-            for (int c = 0; c < 8; ++c) {
-                if (s * 8 + c + kWAhead < KS * 8) read(s * 8 + c + kWAhead);
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wf[(s * 8 + c) % (kWAhead + 1)]), __builtin_bit_cast(bf16x8, af[s % kAhead][r]), acc[c][r], 0, 0, 0);
-                if (c == 7 && (s & 1)) fetch_two((s - 1 + kAhead) % KS);
-                in_this_order();
-            }
+            for (int s = 0; s < kAhead; ++s) fetch(s);
         }
-        // lane: row 16 r + n, columns 16 c + 4 g4 .. + 3
-        constexpr int CK = N / 16;  // column blocks of one of the head's two matrices
+        wait_vm_all();
+        lds_barrier();
+        for (; at < blocks_here; at += 8) {
+            const int64_t row0 = 64ll * (first + from_block + at);
+            f32x4 acc[8][4];
 #pragma unroll
-        for (int part = 0; part < 8 / CK; ++part) {
-            const bool is_v = (set % kSets) * 128 + part * N >= N;
-            float top = 0.f;
+            for (int c = 0; c < 8; ++c)
 #pragma unroll
-            for (int c = part * CK; c < (part + 1) * CK; ++c)
+                for (int r = 0; r < 4; ++r) acc[c][r] = f32x4{0.f, 0.f, 0.f, 0.f};
+            constexpr int kWAhead = 3;
+            u32x4 wf[kWAhead + 1];
+            auto read = [&](int f) __attribute__((always_inline)) {
+                const int s = f >> 3, c = f & 7;
+                wf[f % (kWAhead + 1)] = *reinterpret_cast<__attribute__((address_space(3))) const u32x4*>(lds + w_at[s & 3] + (32 * (c >> 1) + 4 * (c & 1)) * 2 * R + (s >> 2) * 256);
+            };
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
+            for (int f = 0; f < kWAhead; ++f) read(f);
+            in_this_order();
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) top = fmaxf(top, fabsf(acc[c][r][i]));  // (rows behind the last are copies of it)
-            if (__any(top == INFINITY)) {  // (of the finite ones)
-                top = 0.f;
+            for (int s = 0; s < KS; ++s) {
+                if (s + kAhead == KS) point_at(first + from_block + (at + 8 < blocks_here ? at + 8 : at));
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    if (s * 8 + c + kWAhead < KS * 8) read(s * 8 + c + kWAhead);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        acc[c][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wf[(s * 8 + c) % (kWAhead + 1)]), __builtin_bit_cast(bf16x8, af[s % kAhead][r]), acc[c][r], 0, 0, 0);
+                    if (c == 7) fetch((s + kAhead) % KS);
+                    in_this_order();
+                }
+            }
+            products_done();
+            in_this_order();
+            // lane: row 16 r + n, columns 32 p + 8 g4 .. + 7 in c = 2 p, 2 p + 1
+            constexpr int CK = N / 16;  // column blocks of one of the head's two matrices
+#pragma unroll
+            for (int part = 0; part < 8 / CK; ++part) {
+                const bool is_v = (set % kSets) * 128 + part * N >= N;
+                float top = 0.f;
 #pragma unroll
                 for (int c = part * CK; c < (part + 1) * CK; ++c)
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (fabsf(acc[c][r][i]) < INFINITY) top = fmaxf(top, fabsf(acc[c][r][i]));
-            }
-#pragma unroll
-            for (int off = 1; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
-            int e = 0;
-            if (top != 0.f && !(top >= 0.015625f && top < 32768.f)) e = max(min(static_cast<int>(__float_as_uint(top) >> 23) - 127 - 13, 126), -126);
-            if (e != 0) {
-                const float by = power_of_two(-e);
-#pragma unroll
-                for (int c = part * CK; c < (part + 1) * CK; ++c)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[c][r] *= by;
-            }
-            if (row0 < rows && lane == 0) {
-                (is_v ? x.v_exp : x.k_exp)[h * (x.rows_cap / kBlockRows) + row0 / kBlockRows] = static_cast<signed char>(e);
-                if (e != 0) atomicOr(&x.scaled[h0 + h], 1);
-                if (is_v && e > 0) atomicMax(&x.v_top[h0 + h], e);
-            }
-            unsigned short* const to = (is_v ? x.v : x.k) + (h * x.rows_cap + row0) * N;
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (row0 + 16 * r + n < rows)
+                        for (int i = 0; i < 4; i += 2) larger_of(top, acc[c][r][i], acc[c][r][i + 1]);  // (rows behind the last are copies of it)
+                in_this_order();
+                if (__any(top == INFINITY)) [[unlikely]] {  // (of the finite ones)
+                    asm volatile("");  // (a branch, so that nobody else works it out)
+                    top = 0.f;
 #pragma unroll
                     for (int c = part * CK; c < (part + 1) * CK; ++c)
-                        *reinterpret_cast<uint2*>(to + (16 * r + n) * N + (c - part * CK) * 16 + 4 * g4) =
-                            make_uint2(pack_f16x2(acc[c][r][0], acc[c][r][1]), pack_f16x2(acc[c][r][2], acc[c][r][3]));
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if (fabsf(acc[c][r][i]) < INFINITY) top = fmaxf(top, fabsf(acc[c][r][i]));
+                }
+#pragma unroll
+                for (int off = 1; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
+                int e = 0;
+                if (top != 0.f && !(top >= 0.015625f && top < 32768.f)) e = max(min(static_cast<int>(__float_as_uint(top) >> 23) - 127 - 13, 126), -126);
+                if (row0 < rows && lane == 0) {
+                    (is_v ? x.v_exp : x.k_exp)[h * (x.rows_cap / kBlockRows) + row0 / kBlockRows] = static_cast<signed char>(e);
+                    if (e != 0) atomicOr(&x.scaled[h0 + h], 1);
+                    if (is_v && e > 0) atomicMax(&x.v_top[h0 + h], e);
+                }
+                unsigned char* const to = reinterpret_cast<unsigned char*>((is_v ? x.v : x.k) + (h * x.rows_cap + row0) * N);
+                const int rows_here = static_cast<int>(min(rows - row0, static_cast<int64_t>(64)));
+                const unsigned lane_now = worked_out_here(lane), row = lane_now & 15, lane_at = row * (2 * N) + 16 * (lane_now >> 4);
+                // (two copies, so that the sums are read where they are in both)
+                auto store = [&](auto times) __attribute__((always_inline)) {
+                    const float by = power_of_two(-e);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (16 * r + static_cast<int>(row) < rows_here)
+#pragma unroll
+                            for (int c = part * CK; c < (part + 1) * CK; c += 2) {
+                                const f32x4 y = decltype(times)::value ? acc[c][r] * by : acc[c][r], z = decltype(times)::value ? acc[c + 1][r] * by : acc[c + 1][r];
+                                *reinterpret_cast<uint4*>(to + r * (16 * 2 * N) + (c - part * CK) * 32 + lane_at) =
+                                    make_uint4(pack_f16x2(y[0], y[1]), pack_f16x2(y[2], y[3]), pack_f16x2(z[0], z[1]), pack_f16x2(z[2], z[3]));
+                            }
+                };
+                if (__builtin_amdgcn_readfirstlane(e) != 0) store(std::true_type{});
+                else store(std::false_type{});
+            }
         }
     }
 }
@@ -289,8 +321,8 @@ struct ExpShape {
 };
 
 template <int N>
-__global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfloat16* __restrict__ q_ext, LatentBatch b, LatentSplit split, ExpandArgs x, int L,
-                                                                 int H, int h0, float scale_log2e, __hip_bfloat16* __restrict__ out, LatentParts parts) {
+__global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfloat16* __restrict__ q_ext, LatentBatch b, LatentSplit split, ExpandArgs x, int H,
+                                                                 int h0, float scale_log2e, __hip_bfloat16* __restrict__ out, LatentParts parts) {
     using X = ExpShape<N>;
     constexpr int QW = N + kRope, KS = N / 32, KSR = kRope / 32, RB = 2, NB = N / 16;
     constexpr int RPL = 1024 / X::kRow, kRowLoads = 8 / RPL;    // K or V rows of a 1 KB load; loads of a wave's 8 rows
@@ -325,7 +357,7 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
     // the pieces of rows that a lane loads: rows RPL i + lane / (64 / RPL) of the wave's 8, i = 0, 1 (the XOR of i is put to these)
     const int load_row = lane / (64 / RPL), load_piece = lane & (64 / RPL - 1);
     const unsigned k_piece = 16 * (load_piece ^ swz_k<N>((8 * wave + load_row) & 15)), v_piece = 16 * (load_piece ^ swz_v<N>((8 * wave + load_row) & 15));
-    const unsigned r_piece = 2 * (L - kRope) + 16 * ((lane & 7) ^ ((((8 * wave + (lane >> 3)) & 15) >> 1) & 7));
+    const unsigned r_piece = 16 * ((lane & 7) ^ ((((8 * wave + (lane >> 3)) & 15) >> 1) & 7));
 
     bool used[2] = {false, false};
     while (!(at.r == end.r && at.tile == end.tile && at.k == end.k)) {
@@ -365,7 +397,7 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
 #pragma unroll
             for (int i = 0; i < kRowLoads; ++i)
                 load_to_lds_16(k_rows, number(rel, i * RPL + load_row) * X::kRow | (k_piece ^ (64 * i)), lds0 + slot + 8 * wave * X::kRow + i * 1024);
-            load_to_lds_16(x.a, __umul24(number(rel, lane >> 3), 2 * L) + r_piece, lds0 + slot + 2 * X::kK + 8 * wave * 2 * kRope);
+            load_to_lds_16(x.rope, number(rel, lane >> 3) * (2 * kRope) + r_piece, lds0 + slot + 2 * X::kK + 8 * wave * 2 * kRope);
         };
         auto issue_v = [&](int rel, unsigned slot) __attribute__((always_inline)) {
 #pragma unroll
@@ -690,7 +722,7 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
 struct ExpandLayout {
     int heads;  // at once
     int64_t cached_cap, rows_cap;
-    size_t scaled, v_top, map, list, row_of, a, k_exp, v_exp, k, v, parts, total;
+    size_t scaled, v_top, map, list, row_of, a, rope, k_exp, v_exp, k, v, parts, total;
 };
 static ExpandLayout expand_layout(int B, int64_t T, int64_t max_kv_len, int H, int R, int N, int64_t num_slots) {
     ExpandLayout l;
@@ -712,7 +744,8 @@ static ExpandLayout expand_layout(int B, int64_t T, int64_t max_kv_len, int H, i
     l.map = take(sizeof(int32_t) * num_slots);
     l.list = take(sizeof(int32_t) * (l.cached_cap + 1));
     l.row_of = take(sizeof(int32_t) * (listed + 1));
-    l.a = take(static_cast<size_t>(l.rows_cap) * (R + kRope) * 2);
+    l.a = take(static_cast<size_t>(l.rows_cap) * R * 2);
+    l.rope = take(static_cast<size_t>(l.rows_cap) * kRope * 2);
     l.k_exp = take(static_cast<size_t>(l.heads) * (l.rows_cap / kBlockRows));
     l.v_exp = take(static_cast<size_t>(l.heads) * (l.rows_cap / kBlockRows));
     l.k = take(static_cast<size_t>(l.heads) * l.rows_cap * N * 2);
@@ -735,7 +768,7 @@ static int launch_group(const void* q, const LatentBatch& b, const ExpandArgs& x
                         void* out, void* parts_at, hipStream_t stream) {
     {
         ProfScope scope(kProfLatentExpand, stream);
-        hipLaunchKernelGGL((latent_expand_kernel<R, N>), dim3(kExpandWorkgroups), dim3(256), 256 * R, stream, x, static_cast<const __hip_bfloat16*>(w_k),
+        hipLaunchKernelGGL((latent_expand_kernel<R, N>), dim3(kExpandWorkgroups), dim3(512), 256 * R, stream, x, static_cast<const __hip_bfloat16*>(w_k),
                            static_cast<const __hip_bfloat16*>(w_v), b.T, h0, heads);
     }
     PA_HIP(hipGetLastError());
@@ -744,8 +777,8 @@ static int launch_group(const void* q, const LatentBatch& b, const ExpandArgs& x
     parts.hdr = x.hdr;
     {
         ProfScope scope(kProfLatentExpanded, stream);
-        hipLaunchKernelGGL((latent_expanded_kernel<N>), dim3(kExpWorkgroups), dim3(256), ExpShape<N>::kBytes, stream, static_cast<const __hip_bfloat16*>(q), b, split, x,
-                           R + kRope, H, h0, scale * 1.4426950408889634f, static_cast<__hip_bfloat16*>(out), parts);
+        hipLaunchKernelGGL((latent_expanded_kernel<N>), dim3(kExpWorkgroups), dim3(256), ExpShape<N>::kBytes, stream, static_cast<const __hip_bfloat16*>(q), b, split, x, H,
+                           h0, scale * 1.4426950408889634f, static_cast<__hip_bfloat16*>(out), parts);
     }
     PA_HIP(hipGetLastError());
     {
@@ -761,7 +794,7 @@ int latent_expanded_bf16(const void* q, const LatentBatch& b, const void* w_k, c
     const ExpandLayout l = expand_layout(b.B, b.T, max_kv_len, H, R, N, b.num_slots);
     unsigned char* const w = static_cast<unsigned char*>(workspace);
     auto i32 = [&](size_t at) { return reinterpret_cast<int32_t*>(w + at); };
-    const ExpandArgs x = {i32(0), i32(l.scaled), i32(l.v_top), i32(l.map), i32(l.list), i32(l.row_of), reinterpret_cast<__hip_bfloat16*>(w + l.a),
+    const ExpandArgs x = {i32(0), i32(l.scaled), i32(l.v_top), i32(l.map), i32(l.list), i32(l.row_of), reinterpret_cast<uint4*>(w + l.a), reinterpret_cast<uint4*>(w + l.rope),
                           reinterpret_cast<signed char*>(w + l.k_exp), reinterpret_cast<signed char*>(w + l.v_exp), reinterpret_cast<unsigned short*>(w + l.k),
                           reinterpret_cast<unsigned short*>(w + l.v), l.cached_cap, l.rows_cap, static_cast<int>(max_kv_len)};
     {
