@@ -4,10 +4,10 @@
 #include "latent.h"
 
 namespace pa {
-int latent_attention_rows(const void* q, const LatentBatch& b, int H, int R, int dtype, float scale, void* out, hipStream_t stream);
-int latent_expanded_rows(const void* q, const LatentBatch& b, const void* w_k, const void* w_v, int H, int R, int N, int dtype, float scale,
-                         void* out, void* scratch, hipStream_t stream);
-size_t latent_expanded_rows_bytes(int64_t T, int H, int R);
+int latent_attention_f32(const void* q, const LatentBatch& b, int H, int R, float scale, void* out, hipStream_t stream);
+int latent_expanded_f32(const void* q, const LatentBatch& b, const void* w_k, const void* w_v, int H, int R, int N, float scale, void* out, void* scratch,
+                        hipStream_t stream);
+size_t latent_expanded_f32_bytes(int64_t T, int H, int R);
 size_t latent_workspace_bytes_bf16(int B, int64_t T, int64_t max_kv_len, int H, int R);
 int latent_attention_bf16(const void* q, const LatentBatch& b, int64_t max_kv_len, int H, int R, bool kv8, float scale, void* out, void* workspace,
                           hipStream_t stream);
@@ -64,12 +64,12 @@ extern "C" int pa_latent_attention(const void* q_ext, const void* c_ext, const v
     if (nothing) return PA_OK;
     if (dtype != PA_F32)
         return pa::latent_attention_bf16(q_ext, b, max_kv_len, H, R, dtype == PA_BF16_KV8, scale, out, workspace, static_cast<hipStream_t>(stream));
-    return pa::latent_attention_rows(q_ext, b, H, R, dtype, scale, out, static_cast<hipStream_t>(stream));
+    return pa::latent_attention_f32(q_ext, b, H, R, scale, out, static_cast<hipStream_t>(stream));
 }
 
 extern "C" size_t pa_latent_expanded_workspace_bytes(int B, int64_t T, int64_t max_kv_len, int H, int R, int P, int N, int64_t num_slots, int dtype) {
     if (!pa::sizes_ok(B, T, max_kv_len, H, R, P, dtype) || (N != 64 && N != 128) || num_slots <= 0 || num_slots > INT32_MAX) return 0;
-    const size_t n = dtype == PA_F32 ? pa::latent_expanded_rows_bytes(T, H, R) : pa::latent_expanded_bytes(B, T, max_kv_len, H, R, N, num_slots);
+    const size_t n = dtype == PA_F32 ? pa::latent_expanded_f32_bytes(T, H, R) : pa::latent_expanded_bytes(B, T, max_kv_len, H, R, N, num_slots);
     return n == 0 || n >= 256 ? n : 256;
 }
 
@@ -91,5 +91,5 @@ extern "C" int pa_latent_attention_expanded(const void* q_ext, const void* c_ext
     PA_REQUIRE(out != w_k && out != w_v, "%s: out aliases an input", fn);
     if (dtype != PA_F32)
         return pa::latent_expanded_bf16(q_ext, b, w_k, w_v, max_kv_len, H, R, N, dtype == PA_BF16_KV8, scale, out, workspace, static_cast<hipStream_t>(stream));
-    return pa::latent_expanded_rows(q_ext, b, w_k, w_v, H, R, N, dtype, scale, out, workspace, static_cast<hipStream_t>(stream));
+    return pa::latent_expanded_f32(q_ext, b, w_k, w_v, H, R, N, scale, out, workspace, static_cast<hipStream_t>(stream));
 }

@@ -28,6 +28,4 @@ struct LatentBatch {
     int64_t T, num_slots;
 };
 
-int latent_attention_f32(const void* q, const LatentBatch& b, int H, int R, float scale, void* out, hipStream_t stream);
-
 }  // namespace pa
