@@ -53,7 +53,7 @@ __device__ __forceinline__ float power_of_two(int k) { return __int_as_float((k 
 struct ExpandArgs {
     int32_t *hdr;      // [3], [6]: see LatentParts; [8]: distinct cached rows
     int32_t *scaled;   // [H] some block of this head is stored times a power of two
-    int32_t *v_top;    // [H] largest power of two of a block of V
+    int32_t *v_top;    // [2][H] largest power of two but 0 of a block of V; some block has 0
     int32_t *map;      // [num_slots]
     int32_t *list;     // [cached_cap]
     int32_t *row_of;   // [B][max_keys] rows of A of a request's keys, cached and new
@@ -69,12 +69,14 @@ __global__ __launch_bounds__(256) void latent_clear_kernel(ExpandArgs x, int64_t
     for (int64_t i = i0; i < num_slots; i += gridDim.x * 256ll) x.map[i] = -1;
     for (int64_t i = i0; i < H; i += gridDim.x * 256ll) {
         x.scaled[i] = 0;
-        x.v_top[i] = 0;
+        x.v_top[i] = -126;
+        x.v_top[H + i] = 0;
     }
     if (i0 == 0) x.hdr[8] = 0;
 }
 
-// A lane per key of a list.  Which number a slot gets depends on the order of atomics; a row's keys, values and results do not.
+// A lane per key of a list.  Which number a slot gets depends on the order of atomics; a row's keys and values do not, unless its block has a power of two of
+// its own, and then only where they are 2^-28 of the block's largest or less.
 __global__ __launch_bounds__(256) void latent_mark_kernel(LatentBatch b, ExpandArgs x, int chunks) {
     const int r = blockIdx.x / chunks, j = (blockIdx.x - r * chunks) * 256 + threadIdx.x;
     const int P = min(b.prefix_len[r], x.max_keys);
@@ -153,7 +155,7 @@ __global__ __launch_bounds__(256) void latent_collect_kernel(LatentBatch b, Expa
 // without waiting for each other, so that of the two on a SIMD one multiplies while the other packs and stores.
 template <int R, int N>
 __global__ __launch_bounds__(512, 1) void latent_expand_kernel(ExpandArgs x, const __hip_bfloat16* __restrict__ w_k, const __hip_bfloat16* __restrict__ w_v,
-                                                               int64_t T, int h0, int heads) {
+                                                               int64_t T, int h0, int heads, int all_heads) {
     constexpr int KS = R / 32, kSets = 2 * N / 128;  // slices of 32 values; sets of 128 columns per head
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     auto* const lds = (__attribute__((address_space(3))) unsigned char*)smem;
@@ -265,11 +267,16 @@ __global__ __launch_bounds__(512, 1) void latent_expand_kernel(ExpandArgs x, con
 #pragma unroll
                 for (int off = 1; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
                 int e = 0;
-                if (top != 0.f && !(top >= 0.015625f && top < 32768.f)) e = max(min(static_cast<int>(__float_as_uint(top) >> 23) - 127 - 13, 126), -126);
+                if (top == 0.f) e = -126;  // (zeros: of no account beside another block)
+                else if (!(top >= 0.015625f && top < 32768.f)) e = max(min(static_cast<int>(__float_as_uint(top) >> 23) - 127 - 13, 126), -126);
                 if (row0 < rows && lane == 0) {
                     (is_v ? x.v_exp : x.k_exp)[h * (x.rows_cap / kBlockRows) + row0 / kBlockRows] = static_cast<signed char>(e);
-                    if (e != 0) atomicOr(&x.scaled[h0 + h], 1);
-                    if (is_v && e > 0) atomicMax(&x.v_top[h0 + h], e);
+                    if (e != 0 && top != 0.f) {
+                        atomicOr(&x.scaled[h0 + h], 1);
+                        if (is_v) atomicMax(&x.v_top[h0 + h], e);
+                    } else if (is_v && e == 0) {
+                        x.v_top[all_heads + h0 + h] = 1;
+                    }
                 }
                 unsigned char* const to = reinterpret_cast<unsigned char*>((is_v ? x.v : x.k) + (h * x.rows_cap + row0) * N);
                 const int rows_here = static_cast<int>(min(rows - row0, static_cast<int64_t>(64)));
@@ -287,7 +294,7 @@ __global__ __launch_bounds__(512, 1) void latent_expand_kernel(ExpandArgs x, con
                                     make_uint4(pack_f16x2(y[0], y[1]), pack_f16x2(y[2], y[3]), pack_f16x2(z[0], z[1]), pack_f16x2(z[2], z[3]));
                             }
                 };
-                if (__builtin_amdgcn_readfirstlane(e) != 0) store(std::true_type{});
+                if (__builtin_amdgcn_readfirstlane(e) != 0 && top != 0.f) store(std::true_type{});
                 else store(std::false_type{});
             }
         }
@@ -487,6 +494,7 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
         // The tile, with keys and values as they are (the usual case) or with powers of two of their own.
         auto walk = [&](auto scaled_c) __attribute__((always_inline)) {
             constexpr bool scaled = decltype(scaled_c)::value;
+            const int v_top = scaled ? (x.v_top[H + h] ? max(x.v_top[h], 0) : x.v_top[h]) : 0;
             f32x4 sc[2][RB], next[2][RB];  // scores of this step and of the one behind it
             float m[RB], l[RB];
             bool fresh = true, flushed = false;  // fresh: no maxima yet
@@ -504,7 +512,7 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
                 for (int i = 0; i < 4; ++i) {
                     p[i] = __builtin_amdgcn_exp2f(fmaf(sc[kb][rb][i], c[rb], -m[rb]));
                     sum[rb] += p[i];
-                    if constexpr (scaled) p[i] *= power_of_two(max(exponent(x.v_exp, (k0 + rel) * kExpStep + 16 * kb + 4 * g4 + i) - x.v_top[h], -126));
+                    if constexpr (scaled) p[i] *= power_of_two(max(exponent(x.v_exp, (k0 + rel) * kExpStep + 16 * kb + 4 * g4 + i) - v_top, -126));
                 }
                 pw[rb][2 * kb] = worked_out_here(pack_f16x2(p[0], p[1]));  // (here, and not where it is used)
                 pw[rb][2 * kb + 1] = worked_out_here(pack_f16x2(p[2], p[3]));
@@ -671,7 +679,7 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
             const unsigned lane_now = worked_out_here(lane);
             const int n = lane_now & 15, g4 = lane_now >> 4;
             const bool odd_seen = __builtin_amdgcn_readfirstlane(*s_odd) != 0;
-            const float back = scaled ? power_of_two(x.v_top[h]) : 1.f;
+            const float back = scaled ? power_of_two(v_top) : 1.f;
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
                 const float sum = row_sum(l[rb]);
@@ -740,7 +748,7 @@ static ExpandLayout expand_layout(int B, int64_t T, int64_t max_kv_len, int H, i
         return here;
     };
     l.scaled = take(sizeof(int32_t) * H);
-    l.v_top = take(sizeof(int32_t) * H);
+    l.v_top = take(sizeof(int32_t) * 2 * H);
     l.map = take(sizeof(int32_t) * num_slots);
     l.list = take(sizeof(int32_t) * (l.cached_cap + 1));
     l.row_of = take(sizeof(int32_t) * (listed + 1));
@@ -769,7 +777,7 @@ static int launch_group(const void* q, const LatentBatch& b, const ExpandArgs& x
     {
         ProfScope scope(kProfLatentExpand, stream);
         hipLaunchKernelGGL((latent_expand_kernel<R, N>), dim3(kExpandWorkgroups), dim3(512), 256 * R, stream, x, static_cast<const __hip_bfloat16*>(w_k),
-                           static_cast<const __hip_bfloat16*>(w_v), b.T, h0, heads);
+                           static_cast<const __hip_bfloat16*>(w_v), b.T, h0, heads, H);
     }
     PA_HIP(hipGetLastError());
     const LatentSplit split = {1, heads, kExpM, kExpStep, x.max_keys, kExpWorkgroups};
