@@ -11,6 +11,7 @@
 namespace pa {
 
 constexpr int kRope = 64;  // rotary values of a row
+constexpr int kMostGroups = 1 << 20;  // workgroups of a launch with one for each item, at most (a launch has fewer than 2^32 threads)
 
 inline bool latent_shape_ok(int H, int R, int P) { return H > 0 && (R == 256 || R == 512) && P == kRope; }
 

@@ -625,7 +625,7 @@ static int launch_latent(const void* q, const LatentBatch& b, int H, float scale
     PA_HIP(hipGetLastError());
     {
         ProfScope scope(kProfLatentMerge, stream);
-        launch_latent_merge(parts, kWorkgroups, M, R, out, stream);
+        launch_latent_merge(parts, kWorkgroups, M, R, b.T * H, b.B, out, stream);
     }
     PA_HIP(hipGetLastError());
     return PA_OK;

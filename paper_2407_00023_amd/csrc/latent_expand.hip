@@ -78,23 +78,26 @@ __global__ __launch_bounds__(256) void latent_clear_kernel(ExpandArgs x, int64_t
 // A lane per key of a list.  Which number a slot gets depends on the order of atomics; a row's keys and values do not, unless its block has a power of two of
 // its own, and then only where they are 2^-28 of the block's largest or less.
 __global__ __launch_bounds__(256) void latent_mark_kernel(LatentBatch b, ExpandArgs x, int chunks) {
-    const int r = blockIdx.x / chunks, j = (blockIdx.x - r * chunks) * 256 + threadIdx.x;
-    const int P = min(b.prefix_len[r], x.max_keys);
-    bool first = false;
-    int slot = 0;
-    if (j < P && b.ext_len[r] > 0) {
-        slot = static_cast<int>(min(static_cast<int64_t>(max(b.slot_idx[b.slot_offsets[r] + j], 0)), b.num_slots - 1));  // never outside the pool
-        first = x.map[slot] == -1 && atomicCAS(&x.map[slot], -1, -2) == -1;
-    }
-    const unsigned long long all = __ballot(first);
-    if (all == 0) return;
-    const int lane = threadIdx.x & 63, leader = __builtin_ctzll(all);
-    int at = 0;
-    if (lane == leader) at = atomicAdd(&x.hdr[8], __popcll(all));
-    at = __shfl(at, leader) + __popcll(all & ((1ull << lane) - 1));
-    if (first && at < x.cached_cap) {
-        x.list[at] = slot;
-        x.map[slot] = static_cast<int>(b.T) + at;
+    const int64_t pieces = static_cast<int64_t>(b.B) * chunks;
+    for (int64_t piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
+        const int r = static_cast<int>(piece / chunks), j = static_cast<int>(piece - static_cast<int64_t>(r) * chunks) * 256 + threadIdx.x;
+        const int P = min(b.prefix_len[r], x.max_keys);
+        bool first = false;
+        int slot = 0;
+        if (j < P && b.ext_len[r] > 0) {
+            slot = static_cast<int>(min(static_cast<int64_t>(max(b.slot_idx[b.slot_offsets[r] + j], 0)), b.num_slots - 1));  // never outside the pool
+            first = x.map[slot] == -1 && atomicCAS(&x.map[slot], -1, -2) == -1;
+        }
+        const unsigned long long all = __ballot(first);
+        if (all == 0) continue;
+        const int lane = threadIdx.x & 63, leader = __builtin_ctzll(all);
+        int at = 0;
+        if (lane == leader) at = atomicAdd(&x.hdr[8], __popcll(all));
+        at = __shfl(at, leader) + __popcll(all & ((1ull << lane) - 1));
+        if (first && at < x.cached_cap) {
+            x.list[at] = slot;
+            x.map[slot] = static_cast<int>(b.T) + at;
+        }
     }
 }
 
@@ -791,7 +794,7 @@ static int launch_group(const void* q, const LatentBatch& b, const ExpandArgs& x
     PA_HIP(hipGetLastError());
     {
         ProfScope scope(kProfLatentMerge, stream);
-        launch_latent_merge(parts, kExpWorkgroups, kExpM, N, out, stream);
+        launch_latent_merge(parts, kExpWorkgroups, kExpM, N, b.T * heads, static_cast<int64_t>(b.B) * heads, out, stream);
     }
     PA_HIP(hipGetLastError());
     return PA_OK;
@@ -810,7 +813,8 @@ int latent_expanded_bf16(const void* q, const LatentBatch& b, const void* w_k, c
         const int64_t words = b.num_slots > H ? b.num_slots : H, clear = (words + 255) / 256;
         hipLaunchKernelGGL(latent_clear_kernel, dim3(static_cast<unsigned>(clear < 2048 ? clear : 2048)), dim3(256), 0, stream, x, b.num_slots, H);
         const int chunks = static_cast<int>((max_kv_len + 255) / 256);
-        if (chunks > 0) hipLaunchKernelGGL(latent_mark_kernel, dim3(static_cast<unsigned>(b.B) * chunks), dim3(256), 0, stream, b, x, chunks);
+        const int64_t pieces = static_cast<int64_t>(b.B) * chunks;
+        if (pieces > 0) hipLaunchKernelGGL(latent_mark_kernel, dim3(static_cast<unsigned>(pieces < kMostGroups ? pieces : kMostGroups)), dim3(256), 0, stream, b, x, chunks);
         const dim3 grid(2048);
         if (R == 512 && kv8) hipLaunchKernelGGL((latent_collect_kernel<512, true>), grid, dim3(256), 0, stream, b, x);
         else if (R == 512) hipLaunchKernelGGL((latent_collect_kernel<512, false>), grid, dim3(256), 0, stream, b, x);

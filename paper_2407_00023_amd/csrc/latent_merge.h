@@ -10,7 +10,7 @@ namespace pa {
 
 // The parts of tiles joined.  Every workgroup looks at all records, 512 at most, and counts what there is to join, in pieces of kJoinRows rows; the
 // pieces are dealt out in turn.  (A workgroup for every piece that there could be took 40 us to find that most of it had nothing to do.)
-constexpr int kMergeGroups = 2048;  // eight on a compute unit
+constexpr int kMergeGroups = 2048;  // eight on a compute unit, at most
 constexpr int kMaxParts = 512;
 template <int R>
 __global__ __launch_bounds__(256) void latent_merge_kernel(LatentParts parts, int M, int n_max, __hip_bfloat16* __restrict__ out) {
@@ -104,8 +104,10 @@ __global__ __launch_bounds__(256) void latent_merge_kernel(LatentParts parts, in
     }
 }
 
-inline void launch_latent_merge(const LatentParts& parts, int n_wg, int M, int width, void* out, hipStream_t stream) {
-    const dim3 grid(kMergeGroups);
+// rows: of the output, all heads; requests: times the heads that a tile does not hold together
+inline void launch_latent_merge(const LatentParts& parts, int n_wg, int M, int width, int64_t rows, int64_t requests, void* out, hipStream_t stream) {
+    const int64_t pieces = rows / 4 + requests;  // there are no more
+    const dim3 grid(static_cast<unsigned>(pieces < kMergeGroups ? pieces : kMergeGroups));
     __hip_bfloat16* const o = static_cast<__hip_bfloat16*>(out);
     if (width == 512) hipLaunchKernelGGL(latent_merge_kernel<512>, grid, dim3(256), 0, stream, parts, M, n_wg, o);
     else if (width == 256) hipLaunchKernelGGL(latent_merge_kernel<256>, grid, dim3(256), 0, stream, parts, M, n_wg, o);
