@@ -6,19 +6,24 @@
 // much as memory, from two new tokens on the matrix cores.
 //
 // Tiles.  The rows of q of a request (token, head) are one axis, so that a tile of M rows reads every cached row once for all of its heads and
-// tokens.  Four waves, M = 128 or 32.  What decides the layout is the width of the output: 512 fp32 columns for 128 rows are 256 KB, half of a
+// tokens.  Four waves, M = 128, 64 or 32.  What decides the layout is the width of the output: 512 fp32 columns for 128 rows are 256 KB, half of a
 // compute unit's registers, so one workgroup is resident, a wave per SIMD with 512 registers, and the two products are split differently:
-//   scores: a wave computes 32 rows x 32 keys (M = 32: 16 x 16), its rows of Q, all R + kRope of them, in registers;
+//   scores: a wave computes 32 rows x 32 keys (M = 64: 32 x 16, M = 32: 16 x 16), its rows of Q in registers (M = 128: four of 18 slices in LDS);
 //   output: a wave computes all M rows x a quarter of the columns, so that a fragment of C read from LDS is multiplied with eight blocks of
 //           rows; the probabilities go through LDS in between.  (A wave with the output of its own 32 rows would read every fragment of C for
 //           two products only: 68 KB of LDS reads per wave and step instead of 52, and LDS, not the matrix cores, would be the bound.)
 // Scores are computed transposed (S^T = K Q^T): a lane holds one row of q per block and four keys, the output as O^T = C^T P^T, C^T by the
 // transposing LDS read, so that row maxima and sums are per lane and O's rows too.
 //
-// Pipeline.  A step is 32 keys.  In one interval between two barriers a wave computes the scores and probabilities of step i + 1 and the output of
-// step i, and the rows of step i + 3 are on their way from memory straight into LDS, those of step i + 2 landing.  The running maximum of a
-// row only moves when a score outgrows it by kGrow: a wave that sees one sets a flag, and behind the barrier all waves settle on new maxima together
-// (settle()); a probability may reach 2^kGrow until then, which fp32 and bf16 hold as exactly as 1.
+// Pipeline.  A step is 32 keys.  In one interval between two barriers a wave computes the scores of step i + 1, then the output of step i and beside its
+// products the probabilities of step i + 1.  Rows are loaded straight into LDS, two steps ahead of the output (M = 128) or three, their loads set out beside the first
+// products of the scores.  The running maximum of a row moves only when a lane's probabilities of a step sum to more than kMost: the wave that sees it sets a
+// flag, which all waves find in the next interval, and they settle on new maxima together (settle()), the scores computed once more; until then a
+// probability may be as large as kMost, which fp32 and bf16 hold as exactly as 1.
+//
+// Measured: 64 heads, 16 requests of 20 to 80 new tokens over 4 documents of 16 384 rows (1.9 TFLOP): 1850 us, 1.05 PFLOP/s, where a plain product of 16 384
+// squared reaches 1.39; bound by LDS and by waiting beside the matrix cores, which are busy 45 % of the cycles.  128 heads, 128 requests of one token, 500 to 7800 keys: 257 us.
+// 16 heads, 48 requests, 2000 to 24 000 keys of the 8-bit pool: 191 us, 2.5 TB/s, bound by turning codes into bf16.
 //
 // LDS is swizzled in pieces of 16 bytes (swz()) so that reading 16 bytes down 16 rows and the transposing reads of 8 bytes across 8 rows are both
 // free of bank conflicts; direct loads write 1 KB of consecutive LDS, so the swizzle is applied to the address in memory.
@@ -600,11 +605,14 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
 
 constexpr int kWorkgroups = 256;  // one on a compute unit
 
-// Rows of a tile: the fewest that a request's rows fit on the average, 128 at most.
+// Rows of a tile.  No more than a request's rows fill on the average: tiles of 32 rows take 116 us for 128 requests of 16 rows and 500 to 7800 keys, those of 64
+// 142 us, those of 128 238 us; with 64 rows a request it is 214, 158 and 241 us.  Fewer where a workgroup has few keys to go through, since a large tile costs more to
+// begin and to finish: 128 heads, 16 requests of one token and 2133 keys (139 keys a workgroup, in tiles of 128 rows) take 39, 37 and 70 us, 2 requests 31, 41
+// and 62 us; 128 requests of 500 to 7800 keys 398, 278 and 257 us.
 static int tile_rows(int B, int64_t T, int64_t max_kv_len, int H) {
-    (void)max_kv_len;
-    const int64_t rows = T * H;
-    return rows <= 32ll * B ? 32 : rows <= 64ll * B ? 64 : 128;
+    const int64_t rows = T * H, keys = (rows + 127) / 128 * (max_kv_len + kTileCost) / kWorkgroups;  // keys of a workgroup in tiles of 128 rows
+    const int most = rows <= 32ll * B ? 32 : rows <= 64ll * B ? 64 : 128;
+    return keys <= 128 ? 32 : keys <= 1024 && most > 64 ? 64 : most;
 }
 
 size_t latent_workspace_bytes_bf16(int B, int64_t T, int64_t max_kv_len, int H, int R) {

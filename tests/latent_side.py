@@ -2,6 +2,7 @@
 rounding allows.  Shares no code with the library."""
 from __future__ import annotations
 
+import pytest
 import torch
 
 P = 64
@@ -24,8 +25,23 @@ def quantise(c):
     return torch.round(y / step) * step * two_k[:, None], k.int()
 
 
+# The absorbed form goes by tiles of 32, 64 or 128 rows, according to the rows and to how many keys it is told of at most: of 100,000, batches with enough
+# rows take 64, of 10,000,000 as many as their rows fill.
+TOLD = [0, 100_000, 10_000_000]
+FORMS_TOLD = [("absorbed", x) for x in TOLD] + [("expanded", 0)]
+
+
+@pytest.fixture
+def told(request):
+    Batch.told = request.param
+    yield request.param
+    Batch.told = 0
+
+
 class Batch:
     """prefix, ext: lengths per request; share: requests whose cached rows are those of request share[r] as far as they go."""
+
+    told = 0  # keys that the absorbed form is told of, if more than there are
 
     def __init__(self, device, prefix, ext, H, R, dtype=torch.bfloat16, kv8=False, seed=0, num_slots=None, share=None, spread=1.0, gap=0):
         g = torch.Generator().manual_seed(seed)
@@ -64,7 +80,7 @@ class Batch:
         return self.slot_idx, self.offsets, self.prefix_len, self.ext_len, self.ext_offsets, self.scale
 
     def absorbed(self, pa, **kw):
-        kw.setdefault("max_kv_len", self.max_kv_len)
+        kw.setdefault("max_kv_len", max(self.max_kv_len, Batch.told))
         return pa.latent_attention(self.q, self.c, self.pool, *self.batch(), rope_dim=P, **self.kw, **kw)
 
     def weights(self, N, seed=1, std=1.0):

@@ -5,7 +5,7 @@ import threading
 import pytest
 import torch
 
-from latent_side import Batch, P, check, quantise
+from latent_side import FORMS_TOLD, TOLD, Batch, P, check, quantise, told
 
 pytestmark = pytest.mark.gpu
 KINDS = {"f32": (torch.float32, False), "bf16": (torch.bfloat16, False), "bf16_kv8": (torch.bfloat16, True)}
@@ -88,10 +88,11 @@ SHAPES = {  # name: prefix lengths, extend lengths, heads
 }
 
 
+@pytest.mark.parametrize("told", TOLD, indirect=True)
 @pytest.mark.parametrize("R", [512, 256])
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("name", SHAPES)
-def test_absorbed(pa, gpu_device, name, kind, R):
+def test_absorbed(pa, gpu_device, name, kind, R, told):
     dt, kv8 = KINDS[kind]
     prefix, ext, H = SHAPES[name]
     b = Batch(gpu_device, prefix, ext, H, R, dt, kv8, seed=len(name)).fill(pa)
@@ -122,9 +123,9 @@ def test_the_two_forms_are_one(pa, gpu_device, form):
         check(out, ref, bound + 1e-4 * ref.abs().amax())  # (the queries are rounded to fp32 between the two)
 
 
-@pytest.mark.parametrize("form", ["absorbed", "expanded"])
+@pytest.mark.parametrize("form,told", FORMS_TOLD, indirect=["told"])
 @pytest.mark.parametrize("kind", KINDS)
-def test_rows_of_no_request_are_left_alone(pa, gpu_device, kind, form):
+def test_rows_of_no_request_are_left_alone(pa, gpu_device, kind, form, told):
     """Rows before the first request's, between two requests' and behind the last one's stay as they were."""
     dt, kv8 = KINDS[kind]
     b = Batch(gpu_device, [40, 33], [3, 4], 16, 512, dt, kv8, seed=5).fill(pa)
@@ -140,11 +141,11 @@ def test_rows_of_no_request_are_left_alone(pa, gpu_device, kind, form):
     assert bool((out[[0, 1, 5, 10, 11]] == 9.0).all())
 
 
-@pytest.mark.parametrize("form", ["absorbed", "expanded"])
+@pytest.mark.parametrize("form,told", FORMS_TOLD, indirect=["told"])
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("H", [2, 16, 128])
 @pytest.mark.parametrize("value", [float("inf"), float("nan")])
-def test_what_a_row_does_not_see_does_not_reach_it(pa, gpu_device, kind, H, value, form):
+def test_what_a_row_does_not_see_does_not_reach_it(pa, gpu_device, kind, H, value, form, told):
     """A later extend token holds an infinity or NaN: rows before it are what they are without it; so is a request beside it, whose
     cached rows end inside a tile."""
     dt, kv8 = KINDS[kind]
@@ -162,9 +163,10 @@ def test_what_a_row_does_not_see_does_not_reach_it(pa, gpu_device, kind, H, valu
     assert not bool(torch.isfinite(out[21:40].float()).all(-1).any())
 
 
+@pytest.mark.parametrize("told", TOLD, indirect=True)
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("H", [4, 128])
-def test_an_infinity_in_a_cached_row(pa, gpu_device, kind, H):
+def test_an_infinity_in_a_cached_row(pa, gpu_device, kind, H, told):
     """An infinite latent value in the last cached row, with queries that do not look at its place: infinity in its column, for every
     row, and the other columns as ever."""
     dt, kv8 = KINDS[kind]
@@ -183,10 +185,11 @@ def test_an_infinity_in_a_cached_row(pa, gpu_device, kind, H):
     assert bool((out[..., 300] > 1e30).all())
 
 
+@pytest.mark.parametrize("told", TOLD, indirect=True)
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("H", [16, 128])
 @pytest.mark.parametrize("order", ["rising", "falling", "jump"])
-def test_scores_that_outgrow_the_running_maximum(pa, gpu_device, kind, H, order):
+def test_scores_that_outgrow_the_running_maximum(pa, gpu_device, kind, H, order, told):
     dt, kv8 = KINDS[kind]
     b = Batch(gpu_device, [400], [3], H, 512, dt, kv8, seed=9)
     factor = {"rising": torch.linspace(0, 12, 400), "falling": torch.linspace(12, 0, 400), "jump": (torch.arange(400) // 150).float() * 6}[order]
@@ -198,9 +201,9 @@ def test_scores_that_outgrow_the_running_maximum(pa, gpu_device, kind, H, order)
     check(b.absorbed(pa), *b.reference(), f"{order} H {H}")
 
 
-@pytest.mark.parametrize("form", ["absorbed", "expanded"])
+@pytest.mark.parametrize("form,told", FORMS_TOLD, indirect=["told"])
 @pytest.mark.parametrize("kind", KINDS)
-def test_requests_that_share_cached_rows(pa, gpu_device, kind, form):
+def test_requests_that_share_cached_rows(pa, gpu_device, kind, form, told):
     dt, kv8 = KINDS[kind]
     b = Batch(gpu_device, [300, 300, 200, 50, 300], [4, 1, 33, 2, 1], 16, 512, dt, kv8, seed=10, share=[0, 0, 0, 3, 0], gap=3).fill(pa)
     if form == "expanded":
@@ -208,9 +211,9 @@ def test_requests_that_share_cached_rows(pa, gpu_device, kind, form):
     check((b.absorbed if form == "absorbed" else b.expanded)(pa), *b.reference(form))
 
 
-@pytest.mark.parametrize("form", ["absorbed", "expanded"])
+@pytest.mark.parametrize("form,told", FORMS_TOLD, indirect=["told"])
 @pytest.mark.parametrize("kind", KINDS)
-def test_slots_outside_the_pool_are_clamped(pa, gpu_device, kind, form):
+def test_slots_outside_the_pool_are_clamped(pa, gpu_device, kind, form, told):
     """No fault, and requests beside the one with bad slots are what they are."""
     dt, kv8 = KINDS[kind]
     b = Batch(gpu_device, [70, 64], [2, 3], 16, 512, dt, kv8, seed=11).fill(pa)

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from latent_side import Batch, P, check, quantise
+from latent_side import FORMS_TOLD, TOLD, Batch, P, check, quantise, told
 
 pytestmark = pytest.mark.gpu
 KINDS = {"f32": (torch.float32, False), "bf16": (torch.bfloat16, False), "bf16_kv8": (torch.bfloat16, True)}
@@ -40,18 +40,19 @@ def need(pa, b, form, T=None, max_kv_len=None):
 
 # ---- sizes ------------------------------------------------------------------------------------------------------------------
 
+@pytest.mark.parametrize("told", TOLD, indirect=True)
 @pytest.mark.parametrize("R", [256, 512])
 @pytest.mark.parametrize("kind", ["bf16", "bf16_kv8"])
 @pytest.mark.parametrize("H,ext", [(64, 1), (48, 1), (33, 1), (16, 4), (64, 2)])
-def test_tiles_of_64_and_128_rows(pa, gpu_device, kind, R, H, ext):
+def test_tiles_of_64_and_128_rows(pa, gpu_device, kind, R, H, ext, told):
     b = make(pa, gpu_device, [31, 32, 33, 2000, 0, 64], [ext] * 6, H, R, kind, seed=H)
     check(b.absorbed(pa), *b.reference(), f"{H} heads, {ext} tokens, {kind}")
 
 
-@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("form,told", FORMS_TOLD, indirect=["told"])
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("B", [257, 700, 2500])
-def test_many_requests(pa, gpu_device, B, kind, form):
+def test_many_requests(pa, gpu_device, B, kind, form, told):
     """More requests than workgroups, and than a workgroup looks at together; some without extend tokens."""
     g = np.random.default_rng(B)
     prefix, ext = g.integers(0, 90, B).tolist(), g.integers(0, 3, B).tolist()
@@ -59,9 +60,10 @@ def test_many_requests(pa, gpu_device, B, kind, form):
     check(run(pa, b, form), *b.reference(form), f"{B} requests, {kind}, {form}")
 
 
+@pytest.mark.parametrize("told", TOLD, indirect=True)
 @pytest.mark.parametrize("kind", ["bf16", "bf16_kv8"])
 @pytest.mark.parametrize("prefix,ext,H", [([40000], [1], 16), ([30011], [3], 128), ([20000, 3, 17], [1, 1, 2], 5)])
-def test_long_requests_cut_into_many_parts(pa, gpu_device, kind, prefix, ext, H):
+def test_long_requests_cut_into_many_parts(pa, gpu_device, kind, prefix, ext, H, told):
     b = make(pa, gpu_device, prefix, ext, H, kind=kind, seed=H)
     check(b.absorbed(pa), *b.reference(), f"{prefix} cached, {H} heads, {kind}")
     b = make(pa, gpu_device, prefix, ext, min(H, 16), kind=kind, form="expanded", seed=H)
@@ -75,9 +77,9 @@ def test_expanded_heads_in_several_groups(pa, gpu_device):
     check(b.expanded(pa), *b.reference("expanded"), "130 heads, 70 002 rows")
 
 
-@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("form,told", FORMS_TOLD, indirect=["told"])
 @pytest.mark.parametrize("kind", ["bf16", "bf16_kv8"])
-def test_pool_beyond_4_gib(pa, gpu_device, kind, form):
+def test_pool_beyond_4_gib(pa, gpu_device, kind, form, told):
     """Slots on both sides of 4 GiB and at the end of the pool."""
     dt, kv8 = KINDS[kind]
     row = 640 if kv8 else 1152
@@ -130,9 +132,9 @@ def test_expanded_scores_that_outgrow_the_running_maximum(pa, gpu_device, kind, 
 
 # ---- workspaces, streams, graphs -------------------------------------------------------------------------------------------------
 
-@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("form,told", FORMS_TOLD, indirect=["told"])
 @pytest.mark.parametrize("kind", KINDS)
-def test_whatever_the_workspace_holds(pa, gpu_device, kind, form):
+def test_whatever_the_workspace_holds(pa, gpu_device, kind, form, told):
     b = make(pa, gpu_device, [900, 33, 0], [2, 60, 5], 16, kind=kind, form=form, seed=1)
     ref, bound = b.reference(form)
     n = need(pa, b, form)
@@ -142,9 +144,9 @@ def test_whatever_the_workspace_holds(pa, gpu_device, kind, form):
         assert bool((ws[n:] == fill).all())
 
 
-@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("form,told", FORMS_TOLD, indirect=["told"])
 @pytest.mark.parametrize("kind", KINDS)
-def test_two_streams_at_once(pa, gpu_device, kind, form):
+def test_two_streams_at_once(pa, gpu_device, kind, form, told):
     """Two calls at the same time, each with a workspace of its own, on streams other than the current one."""
     bs = [make(pa, gpu_device, [3000, 500], [1, 40], 16, kind=kind, form=form, seed=s) for s in (1, 2)]
     refs = [b.reference(form) for b in bs]
@@ -160,9 +162,9 @@ def test_two_streams_at_once(pa, gpu_device, kind, form):
         check(o, ref, bound, f"{kind}, {form}, on a stream")
 
 
-@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("form,told", FORMS_TOLD, indirect=["told"])
 @pytest.mark.parametrize("kind", KINDS)
-def test_captured_and_replayed(pa, gpu_device, kind, form):
+def test_captured_and_replayed(pa, gpu_device, kind, form, told):
     """Append and attention in one graph, two batches in two graphs on one workspace, replayed in turn with other inputs and eager work between."""
     bs = [make(pa, gpu_device, p, e, 16, kind=kind, form=form, seed=s) for s, (p, e) in enumerate([([700, 0, 90], [1, 3, 1]), ([40, 1500], [30, 1])])]
     ws = torch.zeros(max(need(pa, b, form) for b in bs), dtype=torch.uint8, device=gpu_device)
@@ -191,9 +193,9 @@ def test_captured_and_replayed(pa, gpu_device, kind, form):
             torch.cuda.synchronize()
 
 
-@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("form,told", FORMS_TOLD, indirect=["told"])
 @pytest.mark.parametrize("kind", KINDS)
-def test_same_inputs_same_bits(pa, gpu_device, kind, form):
+def test_same_inputs_same_bits(pa, gpu_device, kind, form, told):
     b = make(pa, gpu_device, [2000, 31, 500], [1, 50, 3], 16, kind=kind, form=form, seed=6, share=[0, 1, 2])
     first = run(pa, b, form).clone()
     for _ in range(4):
