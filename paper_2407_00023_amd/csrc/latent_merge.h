@@ -9,7 +9,7 @@
 namespace pa {
 
 // The parts of tiles joined.  Every workgroup looks at all records, 512 at most, and counts what there is to join, in pieces of kJoinRows rows; the
-// pieces are dealt out in turn.  (A workgroup for every piece that there could be took 40 us to find that most of it had nothing to do.)
+// pieces are dealt out in turn.  12 us with a few parts, of which the launch and three dependent reads are most; 36 us for 20 MB of them.  (A workgroup for every piece that there could be took 40 us to find that most of it had nothing to do.)
 constexpr int kMergeGroups = 2048;  // eight on a compute unit, at most
 constexpr int kMaxParts = 512;
 template <int R>
