@@ -233,16 +233,23 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
             const int j0 = (k0 + rel) * kStep + 8 * wave;
             const unsigned from = X::kCodesAt + (rel & (X::kCodeSlots - 1)) * X::kCodes + 8 * wave * R, exps = X::kExpAt + wave * 64 + (rel & 1) * 32;
             const unsigned to = lat_slot * X::kLat + 8 * wave * X::kLatRow;
+            const int piece = lane & (64 / RPL - 1);
+            u32x2 codes[8 / RPL];
+            signed char k[8 / RPL];
+#pragma unroll
+            for (int i = 0; i < 8 / RPL; ++i) {  // (all reads before the first write: the compiler keeps their order)
+                const int row = i * RPL + lane / (64 / RPL);
+                codes[i] = *reinterpret_cast<__attribute__((address_space(3))) const u32x2*>(lds + from + row * R + 8 * piece);
+                k[i] = *reinterpret_cast<__attribute__((address_space(3))) const signed char*>(lds + exps + 4 * row);
+            }
 #pragma unroll
             for (int i = 0; i < 8 / RPL; ++i) {
-                const int row = i * RPL + lane / (64 / RPL), piece = lane & (64 / RPL - 1);
-                if (j0 + row < P) {
-                    const u32x2 codes = *reinterpret_cast<__attribute__((address_space(3))) const u32x2*>(lds + from + row * R + 8 * piece);
-                    const float two_k = fp8_scale(*reinterpret_cast<__attribute__((address_space(3))) const signed char*>(lds + exps + 4 * row));
-                    const uint2 x = fp8_decode4(codes[0], two_k), y = fp8_decode4(codes[1], two_k);
+                const int row = i * RPL + lane / (64 / RPL);
+                const float two_k = fp8_scale(k[i]);
+                const uint2 x = fp8_decode4(codes[i][0], two_k), y = fp8_decode4(codes[i][1], two_k);
+                if (j0 + row < P)
                     *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(lds + to + row * X::kLatRow + 16 * (piece ^ swz((8 * wave + row) & 15))) =
                         u32x4{x.x, x.y, y.x, y.y};
-                }
             }
         };
 
