@@ -23,7 +23,7 @@
 //
 // Measured: 64 heads, 16 requests of 20 to 80 new tokens over 4 documents of 16 384 rows (1.9 TFLOP): 1850 us, 1.05 PFLOP/s, where a plain product of 16 384
 // squared reaches 1.39; bound by LDS and by waiting beside the matrix cores, which are busy 45 % of the cycles.  128 heads, 128 requests of one token, 500 to 7800 keys: 257 us.
-// 16 heads, 48 requests, 2000 to 24 000 keys of the 8-bit pool: 191 us, 2.5 TB/s, bound by turning codes into bf16.
+// 16 heads, 48 requests, 2000 to 24 000 keys of the 8-bit pool: 176 us, 2.7 TB/s, bound by what a step does outside its products, most of it turning codes into bf16.
 //
 // LDS is swizzled in pieces of 16 bytes (swz()) so that reading 16 bytes down 16 rows and the transposing reads of 8 bytes across 8 rows are both
 // free of bank conflicts; direct loads write 1 KB of consecutive LDS, so the swizzle is applied to the address in memory.
@@ -50,6 +50,10 @@ __device__ __forceinline__ void mfma_first(f32x4& d, bf16x8 a, bf16x8 b) {
 }
 __device__ __forceinline__ void mfma_next(f32x4& d, bf16x8 a, bf16x8 b) {
     asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(d) : "v"(a), "v"(b));
+}
+// ... and one whose result the compiler may move right behind it: the wait is part of it
+__device__ __forceinline__ void mfma_next_done(f32x4& d, bf16x8 a, bf16x8 b) {
+    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0\n\ts_nop 15\n\ts_nop 1" : "+v"(d) : "v"(a), "v"(b));
 }
 __device__ __forceinline__ void products_done() { asm volatile("s_nop 15\n\ts_nop 3" ::: "memory"); }
 
@@ -157,7 +161,9 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
             const unsigned s = min(static_cast<unsigned>(max(slot, 0)), static_cast<unsigned>(b.num_slots - 1));  // never outside the pool
             const uint64_t in_pool = reinterpret_cast<uint64_t>(pool) + static_cast<uint64_t>(s) * PROW;
             const uint64_t in_ext = reinterpret_cast<uint64_t>(c_rows) + static_cast<uint64_t>(max(j - P, 0)) * (2 * L);
-            return j < P ? in_pool : j < key_end ? in_ext : reinterpret_cast<uint64_t>(g_zero_row);
+            uint64_t not_cached = j < key_end ? in_ext : reinterpret_cast<uint64_t>(g_zero_row);
+            if (KV8 && M < 128) asm("" : "+v"(not_cached));  // (chosen, not branched around: a step asks for six addresses here, 16 heads of long requests 181 to 174 us)
+            return j < P ? in_pool : not_cached;
         };
         // slot ids of eight steps from step k0 + 8 blk on, lane: step lane / 8, row lane % 8
         auto load_slots = [&](int blk) {
@@ -234,22 +240,28 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
             const unsigned from = X::kCodesAt + (rel & (X::kCodeSlots - 1)) * X::kCodes + 8 * wave * R, exps = X::kExpAt + wave * 64 + (rel & 1) * 32;
             const unsigned to = lat_slot * X::kLat + 8 * wave * X::kLatRow;
             const int piece = lane & (64 / RPL - 1);
-            u32x2 codes[8 / RPL];
-            signed char k[8 / RPL];
+            // (Reads before the first write, whose order the compiler keeps: all of a step, 16 heads of long requests 191 to 178 us, except in tiles of 128 rows, whose
+            // accumulators leave no registers for it.)
+            constexpr int kTogether = M == 128 ? 1 : 8 / RPL;
 #pragma unroll
-            for (int i = 0; i < 8 / RPL; ++i) {  // (all reads before the first write: the compiler keeps their order)
-                const int row = i * RPL + lane / (64 / RPL);
-                codes[i] = *reinterpret_cast<__attribute__((address_space(3))) const u32x2*>(lds + from + row * R + 8 * piece);
-                k[i] = *reinterpret_cast<__attribute__((address_space(3))) const signed char*>(lds + exps + 4 * row);
-            }
+            for (int i0 = 0; i0 < 8 / RPL; i0 += kTogether) {
+                u32x2 codes[kTogether];
+                signed char k[kTogether];
 #pragma unroll
-            for (int i = 0; i < 8 / RPL; ++i) {
-                const int row = i * RPL + lane / (64 / RPL);
-                const float two_k = fp8_scale(k[i]);
-                const uint2 x = fp8_decode4(codes[i][0], two_k), y = fp8_decode4(codes[i][1], two_k);
-                if (j0 + row < P)
-                    *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(lds + to + row * X::kLatRow + 16 * (piece ^ swz((8 * wave + row) & 15))) =
-                        u32x4{x.x, x.y, y.x, y.y};
+                for (int i = 0; i < kTogether; ++i) {
+                    const int row = (i0 + i) * RPL + lane / (64 / RPL);
+                    codes[i] = *reinterpret_cast<__attribute__((address_space(3))) const u32x2*>(lds + from + row * R + 8 * piece);
+                    k[i] = *reinterpret_cast<__attribute__((address_space(3))) const signed char*>(lds + exps + 4 * row);
+                }
+#pragma unroll
+                for (int i = 0; i < kTogether; ++i) {
+                    const int row = (i0 + i) * RPL + lane / (64 / RPL);
+                    const float two_k = fp8_scale(k[i]);
+                    const uint2 x = fp8_decode4(codes[i][0], two_k), y = fp8_decode4(codes[i][1], two_k);
+                    if (j0 + row < P)
+                        *reinterpret_cast<__attribute__((address_space(3))) u32x4*>(lds + to + row * X::kLatRow + 16 * (piece ^ swz((8 * wave + row) & 15))) =
+                            u32x4{x.x, x.y, y.x, y.y};
+                }
             }
         };
 
@@ -441,14 +453,10 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
                 for (int rb = 0; rb < RB; ++rb) {
                     // (128 rows and 512 columns are all accumulation registers there are; what else the compiler wants some for would cost a block of the
                     // output a place in memory, and a wait for all loads each time: a few blocks have vector registers)
-                    if (RB * NB == 64 && rb == RB - 1 && cb >= NB - kInVector) mfma_next(o[rb][cb], v, pf[rb]);
+                    if (RB * NB == 64 && rb == RB - 1 && cb >= NB - kInVector) mfma_next_done(o[rb][cb], v, pf[rb]);
                     else o[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[rb], o[rb][cb], 0, 0, 0);
                 }
                 if (cb % kEvery == 0) probabilities(rel + 1, (cb / kEvery) % KW, (cb / kEvery) / KW);
-                in_this_order();
-            }
-            if constexpr (RB * NB == 64) {
-                products_done();
                 in_this_order();
             }
         };
@@ -528,7 +536,6 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
                 rope_slot = rope_on(rope_slot, 1);
                 if (rel >= steps) break;
             }
-            products_done();
             if (!grown) {
                 wait_vm_all();  // (nothing is on its way to LDS any more)
                 break;

@@ -308,3 +308,15 @@ def test_profile_names(pa, gpu_device):
         ms, n = pa.profile_read(name)
         assert n >= least and (ms > 0 or n == 0), (name, ms, n)
     pa.profile_enable(False)
+
+
+@pytest.mark.parametrize("told", TOLD, indirect=True)
+@pytest.mark.parametrize("kind", ["bf16", "bf16_kv8"])
+def test_128_heads_many_times_over(pa, gpu_device, kind, told):
+    """Calls behind one another: the same bits every time, within the bound (a result that was read a few cycles too early showed now and then)."""
+    b = make(pa, gpu_device, [100, 1000, 5], [1, 1, 1], 128, kind=kind, seed=17)
+    ref, bound = b.reference()
+    first = b.absorbed(pa).clone()
+    check(first, ref, bound, f"128 heads, {kind}")
+    for _ in range(40):
+        assert torch.equal(bits(b.absorbed(pa)), bits(first))
