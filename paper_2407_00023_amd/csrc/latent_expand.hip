@@ -15,9 +15,10 @@
 // (Waves of 64 rows, one to a SIMD, halve these reads and take longer, 1320 us, since nothing is beside a wave that waits.)
 //
 // fp16 and not bf16, because a rounding of keys, one of values and one of probabilities would each cost as much as the result's own: with 11
-// bits they are an eighth of it each.  What fp16 lacks in range is made up for: a block of 64 rows of K or V of a head whose largest value is out of
-// [2^-6, 2^15) is stored times a power of two, and the attention of that head puts it back (the branch `scaled`, which ordinary values never
-// reach); a row of q is brought to a common size by a power of two, which goes into the factor of its scores.
+// bits they are an eighth of it each.  What fp16 lacks in range is made up for: a row of K or V of a head whose largest value is out of
+// [2^-8, 2^15) is stored times a power of two of its own, and the attention of that head puts it back (the branch `scaled`): what other rows hold, of
+// other requests or of none, and where a row lies, decide nothing about it.  A row of q is brought to a common size by a power of two, which goes into the
+// factor of its scores.
 #include <hip/hip_bf16.h>
 #include <hip/hip_fp16.h>
 
@@ -48,7 +49,8 @@ constexpr int kExpandWorkgroups = 256;  // one on a compute unit
 constexpr int kExpWorkgroups = 512;     // two
 constexpr int kExpM = 128;           // rows of q of a tile
 constexpr int kExpStep = 32;         // keys of a step
-constexpr int kBlockRows = 64;       // rows of K or V with one power of two
+constexpr int kExpLow = -8;          // a row of K or V is stored as it is if its largest value is in [2^kExpLow, 2^15)
+constexpr int kBlockRows = 64;       // rows of K or V that a wave of the expansion makes at a time
 
 __device__ __forceinline__ unsigned pack_f16x2(float a, float b) {
     return __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2_t{a, b}), f16x2));
@@ -57,13 +59,12 @@ __device__ __forceinline__ float power_of_two(int k) { return __int_as_float((k 
 
 struct ExpandArgs {
     int32_t *hdr;      // [3], [6]: see LatentParts; [8]: distinct cached rows
-    int32_t *scaled;   // [H] some block of this head is stored times a power of two
-    int32_t *v_top;    // [2][H] largest power of two but 0 of a block of V; some block has 0
+    int32_t *scaled;   // [H] some row of K or V of this head is stored times a power of two
     int32_t *map;      // [num_slots]
     int32_t *list;     // [cached_cap]
     int32_t *row_of;   // [B][max_keys] rows of A of a request's keys, cached and new
     uint4 *a, *rope;   // latent parts [rows_cap / 16][R / 32][64 lanes], as fragments (see collect); rotary parts [rows_cap][8]
-    signed char *k_exp, *v_exp;  // [heads at once][rows_cap / 64]
+    signed char *k_exp, *v_exp;  // [heads at once][rows_cap] a row is what is stored times 2^this
     unsigned short *k, *v;       // [heads at once][rows_cap][N] fp16
     int64_t cached_cap, rows_cap;
     int max_keys;
@@ -72,16 +73,11 @@ struct ExpandArgs {
 __global__ __launch_bounds__(256) void latent_clear_kernel(ExpandArgs x, int64_t num_slots, int H) {
     const int64_t i0 = blockIdx.x * 256ll + threadIdx.x;
     for (int64_t i = i0; i < num_slots; i += gridDim.x * 256ll) x.map[i] = -1;
-    for (int64_t i = i0; i < H; i += gridDim.x * 256ll) {
-        x.scaled[i] = 0;
-        x.v_top[i] = -126;
-        x.v_top[H + i] = 0;
-    }
+    for (int64_t i = i0; i < H; i += gridDim.x * 256ll) x.scaled[i] = 0;
     if (i0 == 0) x.hdr[8] = 0;
 }
 
-// A lane per key of a list.  Which number a slot gets depends on the order of atomics; a row's keys and values do not, unless its block has a power of two of
-// its own, and then only where they are 2^-28 of the block's largest or less.
+// A lane per key of a list.  Which number a slot gets depends on the order of atomics; a row's keys and values do not, wherever they lie.
 __global__ __launch_bounds__(256) void latent_mark_kernel(LatentBatch b, ExpandArgs x, int chunks) {
     const int64_t pieces = static_cast<int64_t>(b.B) * chunks;
     for (int64_t piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
@@ -163,7 +159,7 @@ __global__ __launch_bounds__(256) void latent_collect_kernel(LatentBatch b, Expa
 // without waiting for each other, so that of the two on a SIMD one multiplies while the other packs and stores.
 template <int R, int N>
 __global__ __launch_bounds__(512, 1) void latent_expand_kernel(ExpandArgs x, const __hip_bfloat16* __restrict__ w_k, const __hip_bfloat16* __restrict__ w_v,
-                                                               int64_t T, int h0, int heads, int all_heads) {
+                                                               int64_t T, int h0, int heads) {
     constexpr int KS = R / 32, kSets = 2 * N / 128;  // slices of 32 values; sets of 128 columns per head
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     auto* const lds = (__attribute__((address_space(3))) unsigned char*)smem;
@@ -253,56 +249,51 @@ __global__ __launch_bounds__(512, 1) void latent_expand_kernel(ExpandArgs x, con
 #pragma unroll
             for (int part = 0; part < 8 / CK; ++part) {
                 const bool is_v = (set % kSets) * 128 + part * N >= N;
-                float top = 0.f;
+                // The exponents of the rows 16 r + n, a byte for every r.  A row whose largest value is out of [2^kExpLow, 2^15) is brought to the edge of that
+                // range, no further: a product of one stored as it is and one that is not then differ by as little as can be.  (0 otherwise, and for zeros.)
+                unsigned e = 0;
 #pragma unroll
-                for (int c = part * CK; c < (part + 1) * CK; ++c)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-#pragma unroll
-                        for (int i = 0; i < 4; i += 2) larger_of(top, acc[c][r][i], acc[c][r][i + 1]);  // (rows behind the last are copies of it)
-                in_this_order();
-                if (__any(top == INFINITY)) [[unlikely]] {  // (of the finite ones)
-                    asm volatile("");  // (a branch, so that nobody else works it out)
-                    top = 0.f;
+                for (int r = 0; r < 4; ++r) {
+                    float top = 0.f;
 #pragma unroll
                     for (int c = part * CK; c < (part + 1) * CK; ++c)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
+                        for (int i = 0; i < 4; i += 2) larger_of(top, acc[c][r][i], acc[c][r][i + 1]);
+                    in_this_order();
+                    if (__any(top == INFINITY)) [[unlikely]] {  // (of the finite ones)
+                        asm volatile("");  // (a branch, so that nobody else works it out)
+                        top = 0.f;
+#pragma unroll
+                        for (int c = part * CK; c < (part + 1) * CK; ++c)
 #pragma unroll
                             for (int i = 0; i < 4; ++i)
                                 if (fabsf(acc[c][r][i]) < INFINITY) top = fmaxf(top, fabsf(acc[c][r][i]));
-                }
-#pragma unroll
-                for (int off = 1; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
-                int e = 0;
-                if (top == 0.f) e = -126;  // (zeros: of no account beside another block)
-                else if (!(top >= 0.015625f && top < 32768.f)) e = max(min(static_cast<int>(__float_as_uint(top) >> 23) - 127 - 13, 126), -126);
-                if (row0 < rows && lane == 0) {
-                    (is_v ? x.v_exp : x.k_exp)[h * (x.rows_cap / kBlockRows) + row0 / kBlockRows] = static_cast<signed char>(e);
-                    if (e != 0 && top != 0.f) {
-                        atomicOr(&x.scaled[h0 + h], 1);
-                        if (is_v) atomicMax(&x.v_top[h0 + h], e);
-                    } else if (is_v && e == 0) {
-                        x.v_top[all_heads + h0 + h] = 1;
                     }
+                    top = row_max(top);
+                    const int log2_top = static_cast<int>(__float_as_uint(top) >> 23) - 127;
+                    if (top != 0.f) e |= static_cast<unsigned>(max(log2_top - 14, min(log2_top - kExpLow, 0)) & 255) << (8 * r);
                 }
+                const unsigned lane_now = worked_out_here(lane);
+                (is_v ? x.v_exp : x.k_exp)[h * x.rows_cap + row0 + lane_now] = static_cast<signed char>(e >> (8 * (lane_now >> 4)));
+                const bool any_scaled = __any(e != 0);
+                if (any_scaled && lane == 0) x.scaled[h0 + h] = 1;
                 unsigned char* const to = reinterpret_cast<unsigned char*>((is_v ? x.v : x.k) + (h * x.rows_cap + row0) * N);
                 const int rows_here = static_cast<int>(min(rows - row0, static_cast<int64_t>(64)));
-                const unsigned lane_now = worked_out_here(lane), row = lane_now & 15, lane_at = row * (2 * N) + 16 * (lane_now >> 4);
+                const unsigned row = lane_now & 15, lane_at = row * (2 * N) + 16 * (lane_now >> 4);
                 // (two copies, so that the sums are read where they are in both)
                 auto store = [&](auto times) __attribute__((always_inline)) {
-                    const float by = power_of_two(-e);
 #pragma unroll
                     for (int r = 0; r < 4; ++r)
                         if (16 * r + static_cast<int>(row) < rows_here)
 #pragma unroll
                             for (int c = part * CK; c < (part + 1) * CK; c += 2) {
+                                const float by = power_of_two(-static_cast<int>(static_cast<signed char>(e >> (8 * r))));
                                 const f32x4 y = decltype(times)::value ? acc[c][r] * by : acc[c][r], z = decltype(times)::value ? acc[c + 1][r] * by : acc[c + 1][r];
                                 *reinterpret_cast<uint4*>(to + r * (16 * 2 * N) + (c - part * CK) * 32 + lane_at) =
                                     make_uint4(pack_f16x2(y[0], y[1]), pack_f16x2(y[2], y[3]), pack_f16x2(z[0], z[1]), pack_f16x2(z[2], z[3]));
                             }
                 };
-                if (__builtin_amdgcn_readfirstlane(e) != 0 && top != 0.f) store(std::true_type{});
+                if (any_scaled) store(std::true_type{});
                 else store(std::false_type{});
             }
         }
@@ -331,7 +322,8 @@ constexpr int kExpSlots = 3;
 
 template <int N>
 struct ExpShape {
-    static constexpr int kRow = 2 * N, kK = kExpStep * kRow, kR = kExpStep * 2 * kRope, kSlot = 2 * kK + kR;
+    static constexpr int kRow = 2 * N, kK = kExpStep * kRow, kR = kExpStep * 2 * kRope;
+    static constexpr int kKExp = 2 * kK + kR, kVExp = kKExp + 4 * kExpStep, kSlot = kVExp + 4 * kExpStep;  // (exponents: a word per row)
     static constexpr int kRowsAt = kExpSlots * kSlot, kOddAt = kRowsAt + 4 * 2 * 256, kBytes = kOddAt + 16;
 };
 
@@ -408,16 +400,22 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
         auto number = [&](int rel, int row) __attribute__((always_inline)) {
             return *reinterpret_cast<__attribute__((address_space(3))) const unsigned*>(lds + X::kRowsAt + wave * 512 + (rel & 15) * 32 + 4 * row);
         };
-        auto issue_k = [&](int rel, unsigned slot) __attribute__((always_inline)) {
+        // (with_exps: the rows' powers of two too, a load more)
+        auto issue_exps = [&](const signed char* of, int rel, unsigned to) __attribute__((always_inline)) {
+            if (lane < 8) load_to_lds_1(of + copy * x.rows_cap + number(rel, lane), lds0 + to + 32 * wave);
+        };
+        auto issue_k = [&](int rel, unsigned slot, auto with_exps) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < kRowLoads; ++i)
                 load_to_lds_16(k_rows, number(rel, i * RPL + load_row) * X::kRow | (k_piece ^ (64 * i)), lds0 + slot + 8 * wave * X::kRow + i * 1024);
             load_to_lds_16(x.rope, number(rel, lane >> 3) * (2 * kRope) + r_piece, lds0 + slot + 2 * X::kK + 8 * wave * 2 * kRope);
+            if constexpr (decltype(with_exps)::value) issue_exps(x.k_exp, rel, slot + X::kKExp);
         };
-        auto issue_v = [&](int rel, unsigned slot) __attribute__((always_inline)) {
+        auto issue_v = [&](int rel, unsigned slot, auto with_exps) __attribute__((always_inline)) {
 #pragma unroll
             for (int i = 0; i < kRowLoads; ++i)
                 load_to_lds_16(v_rows, number(rel, i * RPL + load_row) * X::kRow | (v_piece ^ (32 * i)), lds0 + slot + X::kK + 8 * wave * X::kRow + i * 1024);
+            if constexpr (decltype(with_exps)::value) issue_exps(x.v_exp, rel, slot + X::kVExp);
         };
 
         // Steps with keys that some row of the tile does not see, or behind the last: 0 times an infinity or NaN of such a key would be NaN.  The wave
@@ -483,61 +481,72 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
         }
         wait_vm_all();
         load_row_numbers(1);
-        issue_k(0, 0);
-        issue_v(0, 0);
-        if (steps > 1) issue_k(1, X::kSlot);
-        if (steps > 1) issue_v(1, X::kSlot);
-        if (steps > 2) issue_k(2, 2 * X::kSlot);
-        if (steps > 2) wait_vm<kLoads>();
-        else if (steps > 1) wait_vm<kRowLoads>();
-        else wait_vm_all();
         if (tid == 0) *s_odd = 0;
-        lds_barrier();
-        clean(0, 0);
-        lds_barrier();
 
         const bool head = k0 == 0, last = k1 == all_steps, whole = head && last;
         const int part = 2 * wl + (head ? 1 : 0);
         const int out_row0 = (e0 + row0) * H + h;
-        // The tile, with keys and values as they are (the usual case) or with powers of two of their own.
+        // The tile, with keys and values as they are (the usual case) or with powers of two of their own, 2^a of a key and 2^b of a value.  A key's comes into its
+        // score.  A value's goes with its probability, which is then measured against a maximum of its own: with z the score in log2 units, m the running
+        // maximum of z and w that of z + b,   sum = sum 2^(z - m),   O = sum 2^(z + b - w) V,   out = 2^(w - m) O / sum.   What a product with V is worth beside
+        // the others decides so how many bits its probability has, however far apart the sizes are; with b = 0 throughout every number is what it is without.
         auto walk = [&](auto scaled_c) __attribute__((always_inline)) {
             constexpr bool scaled = decltype(scaled_c)::value;
-            const int v_top = scaled ? (x.v_top[H + h] ? max(x.v_top[h], 0) : x.v_top[h]) : 0;
+            constexpr int kVLoads = kRowLoads + scaled, kKVLoads = kLoads + 2 * scaled;
+            issue_k(0, 0, scaled_c);
+            issue_v(0, 0, scaled_c);
+            if (steps > 1) issue_k(1, X::kSlot, scaled_c);
+            if (steps > 1) issue_v(1, X::kSlot, scaled_c);
+            if (steps > 2) issue_k(2, 2 * X::kSlot, scaled_c);
+            if (steps > 2) wait_vm<kKVLoads>();
+            else if (steps > 1) wait_vm<kVLoads>();
+            else wait_vm_all();
+            lds_barrier();
+            clean(0, 0);
+            lds_barrier();
             f32x4 sc[2][RB], next[2][RB];  // scores of this step and of the one behind it
             float m[RB], l[RB];
+            float w[RB], sum_w[RB];              // (scaled) the maxima of z + b, sums of the probabilities that V is multiplied with
             bool fresh = true, flushed = false;  // fresh: no maxima yet
-            // the power of two of a key's or value's block
-            auto exponent = [&](const signed char* of, int j) -> int {
-                return j >= key_end ? 0 : of[copy * (x.rows_cap / kBlockRows) + row_of[j] / kBlockRows];
+            unsigned slot = 0;  // of step rel
+            // the exponents of the keys or values 16 kb + 4 g4 .. + 3 of a step
+            auto exponents = [&](unsigned at, int kb) __attribute__((always_inline)) {
+                return *reinterpret_cast<__attribute__((address_space(3))) const u32x4*>(lds + at + 64 * kb + 16 * g4);
             };
+            auto exponent = [](unsigned word) { return static_cast<int>(static_cast<signed char>(word)); };
             // a quarter of the probabilities of the scores of step rel, [rb][kb], and their sums
             f16x8 pr[RB];
             unsigned pw[RB][4];
             float sum[RB];
-            auto probabilities = [&](int rel, int kb, int rb) __attribute__((always_inline)) {
+            auto probabilities = [&](int kb, int rb) __attribute__((always_inline)) {
                 float p[4];
+                u32x4 b = {0, 0, 0, 0};
+                if constexpr (scaled) b = exponents(slot + X::kVExp, kb);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     p[i] = __builtin_amdgcn_exp2f(fmaf(sc[kb][rb][i], c[rb], -m[rb]));
                     sum[rb] += p[i];
-                    if constexpr (scaled) p[i] *= power_of_two(max(exponent(x.v_exp, (k0 + rel) * kExpStep + 16 * kb + 4 * g4 + i) - v_top, -126));
+                    if constexpr (scaled) {
+                        p[i] = __builtin_amdgcn_exp2f(fmaf(sc[kb][rb][i], c[rb], exponent(b[i]) - w[rb]));
+                        sum_w[rb] += p[i];
+                    }
                 }
                 pw[rb][2 * kb] = worked_out_here(pack_f16x2(p[0], p[1]));  // (here, and not where it is used)
                 pw[rb][2 * kb + 1] = worked_out_here(pack_f16x2(p[2], p[3]));
             };
-            // The scores of step rel + 1 into `next`, and beside them the probabilities of step rel: a piece of these behind every few products.
+            // The scores of a step into `next`, and beside them the probabilities of the step before, whose scores are at hand: a piece of these behind every few products.
             // Fragments are read four ahead.
             constexpr int kFrags = 2 * (KS + KSR), kAhead = 4;
-            auto scores = [&](int rel1, unsigned slot, auto with) __attribute__((always_inline)) {
+            auto scores = [&](int rel1, unsigned slot1, auto with) __attribute__((always_inline)) {
                 constexpr bool probs = decltype(with)::value;
 #pragma unroll
-                for (int rb = 0; rb < RB; ++rb) sum[rb] = 0.f;
+                for (int rb = 0; rb < RB; ++rb) sum[rb] = sum_w[rb] = 0.f;
                 const int j0 = (k0 + rel1) * kExpStep;
                 u32x4 kf[kFrags];
                 auto read = [&](int f) __attribute__((always_inline)) {
                     const int s = f >> 1, kb = f & 1;
                     kf[f] = *reinterpret_cast<__attribute__((address_space(3))) const u32x4*>(
-                        lds + (s < KS ? k_at[s] + kb * 16 * X::kRow : r_at[s - KS] + kb * 16 * 2 * kRope) + slot);
+                        lds + (s < KS ? k_at[s] + kb * 16 * X::kRow : r_at[s - KS] + kb * 16 * 2 * kRope) + slot1);
                 };
 #pragma unroll
                 for (int f = 0; f < kAhead; ++f) read(f);
@@ -547,13 +556,13 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
                     const int s = f >> 1, kb = f & 1;
                     if (scaled && f == 2 * KS) {
 #pragma unroll
-                        for (int y = 0; y < 2; ++y)
+                        for (int y = 0; y < 2; ++y) {
+                            const u32x4 a = exponents(slot1 + X::kKExp, y);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const float by = power_of_two(exponent(x.k_exp, j0 + 16 * y + 4 * g4 + i));
+                            for (int i = 0; i < 4; ++i)
 #pragma unroll
-                                for (int rb = 0; rb < RB; ++rb) next[y][rb][i] *= by;
-                            }
+                                for (int rb = 0; rb < RB; ++rb) next[y][rb][i] *= power_of_two(exponent(a[i]));
+                        }
                     }
 #pragma unroll
                     for (int rb = 0; rb < RB; ++rb) {
@@ -564,7 +573,7 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
                     if (f + kAhead < kFrags) read(f + kAhead);
                     if constexpr (probs) {
                         constexpr int kEvery = kFrags / 4;
-                        if (f % kEvery == 0 && f / kEvery < 4) probabilities(rel1 - 1, (f / kEvery) & 1, (f / kEvery) >> 1);
+                        if (f % kEvery == 0 && f / kEvery < 4) probabilities((f / kEvery) & 1, (f / kEvery) >> 1);
                     }
                     in_this_order();
                 }
@@ -587,6 +596,16 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
 #pragma unroll
                     for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[kb][rb][i]);
                 return mx * c[rb];
+            };
+            auto largest_w = [&](int rb) __attribute__((always_inline)) {
+                float mx = -INFINITY;
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    const u32x4 b = exponents(slot + X::kVExp, kb);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) mx = fmaxf(mx, fmaf(sc[kb][rb][i], c[rb], static_cast<float>(exponent(b[i]))));
+                }
+                return mx;
             };
             auto take_next = [&]() __attribute__((always_inline)) {
 #pragma unroll
@@ -622,10 +641,9 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
             };
 
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb) m[rb] = l[rb] = 0.f;
+            for (int rb = 0; rb < RB; ++rb) m[rb] = l[rb] = w[rb] = 0.f;
             int rel = 0;
             f32x4 o[RB][NB];
-            unsigned slot = 0;  // of step rel; the two behind it
             auto behind = [](unsigned x) { return x == 2 * X::kSlot ? 0u : x + X::kSlot; };
             scores(0, 0, std::false_type{});
             take_next();
@@ -640,18 +658,18 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
                     scores(rel + 1, slot1, std::true_type{});  // (behind the last step: of whatever lies there, not used)
                     bool outgrown = false;
 #pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) outgrown |= sum[rb] > kExpMost;
+                    for (int rb = 0; rb < RB; ++rb) outgrown |= sum[rb] > kExpMost || (scaled && sum_w[rb] > kExpMost);
                     grown = __any(outgrown);
                     if (grown) break;
 #pragma unroll
                     for (int rb = 0; rb < RB; ++rb) l[rb] += sum[rb];
                     if ((rel & 7) == 6) load_row_numbers((rel + 2) / 8 + 1);
-                    if (rel + 2 < steps) issue_v(rel + 2, slot2);
-                    if (rel + 3 < steps) issue_k(rel + 3, slot);
+                    if (rel + 2 < steps) issue_v(rel + 2, slot2, scaled_c);
+                    if (rel + 3 < steps) issue_k(rel + 3, slot, scaled_c);
                     output(slot, o);
                     take_next();
-                    if (rel + 3 < steps) wait_vm<kLoads>();
-                    else if (rel + 2 < steps) wait_vm<kRowLoads>();
+                    if (rel + 3 < steps) wait_vm<kKVLoads>();
+                    else if (rel + 2 < steps) wait_vm<kVLoads>();
                     else wait_vm_all();
                     if (rel + 1 < steps) clean(rel + 1, slot1);
                     lds_barrier();
@@ -666,13 +684,19 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
                         const float mx = row_max(largest(rb));
                         const float mn = fresh ? (mx == -INFINITY ? 0.f : mx) : fmaxf(mx, m[rb]);  // (a row that sees no key yet sees none at all)
                         const float a = fresh ? 0.f : __builtin_amdgcn_exp2f(m[rb] - mn);
+                        float a_w = a;  // of what V was multiplied with
+                        if constexpr (scaled) {
+                            const float mx_w = row_max(largest_w(rb)), wn = fresh ? (mx_w == -INFINITY ? 0.f : mx_w) : fmaxf(mx_w, w[rb]);
+                            a_w = __builtin_amdgcn_exp2f(w[rb] - wn);
+                            w[rb] = wn;
+                        }
                         if (!fresh) {
                             float* const to = scratch(worked_out_here(lane)) + 16 * rb * N;
 #pragma unroll
                             for (int cb = 0; cb < NB; ++cb) {
                                 f32x4 y = o[rb][cb];
                                 if (flushed) y += *reinterpret_cast<const f32x4*>(to + 16 * cb);
-                                *reinterpret_cast<f32x4*>(to + 16 * cb) = y * a;
+                                *reinterpret_cast<f32x4*>(to + 16 * cb) = y * a_w;
                             }
                         }
                         l[rb] *= a;
@@ -687,7 +711,6 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
             const unsigned lane_now = worked_out_here(lane);
             const int n = lane_now & 15, g4 = lane_now >> 4;
             const bool odd_seen = __builtin_amdgcn_readfirstlane(*s_odd) != 0;
-            const float back = scaled ? power_of_two(v_top) : 1.f;
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb) {
                 const float sum = row_sum(l[rb]);
@@ -700,7 +723,7 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
                     f32x4 y = o[rb][cb];
                     if (flushed) y += *reinterpret_cast<const f32x4*>(scratch(lane_now) + 16 * rb * N + 16 * cb);
                     y *= inv;
-                    if constexpr (scaled) y *= back;
+                    if constexpr (scaled) y *= __builtin_amdgcn_exp2f(w[rb] - m[rb]);
                     const int col = 16 * cb + 4 * g4;
                     if (odd_seen) {
                         // (a weight is positive: an infinity stays one, two of opposite sign and NaN give NaN; the keys of the steps they were taken out of)
@@ -738,7 +761,7 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
 struct ExpandLayout {
     int heads;  // at once
     int64_t cached_cap, rows_cap;
-    size_t scaled, v_top, map, list, row_of, a, rope, k_exp, v_exp, k, v, parts, total;
+    size_t scaled, map, list, row_of, a, rope, k_exp, v_exp, k, v, parts, total;
 };
 static ExpandLayout expand_layout(int B, int64_t T, int64_t max_kv_len, int H, int R, int N, int64_t num_slots) {
     ExpandLayout l;
@@ -756,14 +779,13 @@ static ExpandLayout expand_layout(int B, int64_t T, int64_t max_kv_len, int H, i
         return here;
     };
     l.scaled = take(sizeof(int32_t) * H);
-    l.v_top = take(sizeof(int32_t) * 2 * H);
     l.map = take(sizeof(int32_t) * num_slots);
     l.list = take(sizeof(int32_t) * (l.cached_cap + 1));
     l.row_of = take(sizeof(int32_t) * (listed + 1));
     l.a = take(static_cast<size_t>(l.rows_cap) * R * 2);
     l.rope = take(static_cast<size_t>(l.rows_cap) * kRope * 2);
-    l.k_exp = take(static_cast<size_t>(l.heads) * (l.rows_cap / kBlockRows));
-    l.v_exp = take(static_cast<size_t>(l.heads) * (l.rows_cap / kBlockRows));
+    l.k_exp = take(static_cast<size_t>(l.heads) * l.rows_cap);
+    l.v_exp = take(static_cast<size_t>(l.heads) * l.rows_cap);
     l.k = take(static_cast<size_t>(l.heads) * l.rows_cap * N * 2);
     l.v = take(static_cast<size_t>(l.heads) * l.rows_cap * N * 2);
     l.parts = take(latent_parts_layout(kExpWorkgroups, kExpM, N).total);
@@ -785,7 +807,7 @@ static int launch_group(const void* q, const LatentBatch& b, const ExpandArgs& x
     {
         ProfScope scope(kProfLatentExpand, stream);
         hipLaunchKernelGGL((latent_expand_kernel<R, N>), dim3(kExpandWorkgroups), dim3(512), 256 * R, stream, x, static_cast<const __hip_bfloat16*>(w_k),
-                           static_cast<const __hip_bfloat16*>(w_v), b.T, h0, heads, H);
+                           static_cast<const __hip_bfloat16*>(w_v), b.T, h0, heads);
     }
     PA_HIP(hipGetLastError());
     const LatentSplit split = {1, heads, kExpM, kExpStep, x.max_keys, kExpWorkgroups};
@@ -810,7 +832,7 @@ int latent_expanded_bf16(const void* q, const LatentBatch& b, const void* w_k, c
     const ExpandLayout l = expand_layout(b.B, b.T, max_kv_len, H, R, N, b.num_slots);
     unsigned char* const w = static_cast<unsigned char*>(workspace);
     auto i32 = [&](size_t at) { return reinterpret_cast<int32_t*>(w + at); };
-    const ExpandArgs x = {i32(0), i32(l.scaled), i32(l.v_top), i32(l.map), i32(l.list), i32(l.row_of), reinterpret_cast<uint4*>(w + l.a), reinterpret_cast<uint4*>(w + l.rope),
+    const ExpandArgs x = {i32(0), i32(l.scaled), i32(l.map), i32(l.list), i32(l.row_of), reinterpret_cast<uint4*>(w + l.a), reinterpret_cast<uint4*>(w + l.rope),
                           reinterpret_cast<signed char*>(w + l.k_exp), reinterpret_cast<signed char*>(w + l.v_exp), reinterpret_cast<unsigned short*>(w + l.k),
                           reinterpret_cast<unsigned short*>(w + l.v), l.cached_cap, l.rows_cap, static_cast<int>(max_kv_len)};
     {
