@@ -34,6 +34,7 @@ namespace pa {
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
@@ -316,8 +317,11 @@ __device__ __forceinline__ int swz_v(int row) {
 // In the loop the scores of step i + 1 and the output of step i are computed, the probabilities of step i in between; keys of step i + 3 and values of
 // step i + 2 are on their way to LDS, each in a ring of three.  A row's maximum moves when a lane's probabilities of a step sum to more than kExpMost: the wave leaves
 // the loop, what it has summed up goes to memory, multiplied accordingly, and the accumulators begin anew (inside the loop the compiler
-// would keep a second copy of them).
+// would keep a second copy of them).  A maximum so large that its rounding shows (moved_maximum()) does not help the step it was taken from: if a step makes the
+// wave leave the loop a second time, its probabilities are worked out there, held to 2^kExpCap, and the loop goes on whatever they sum to.
 constexpr float kExpMost = 16384.f;  // 2^14 is a large fp16 still
+constexpr unsigned short kHalfMost = 0x7400, kHalfInfinity = 0x7C00;  // kExpMost and infinity in fp16
+constexpr float kExpCap = 11.f;      // log2 of what probabilities are held to then: eight of them are kExpMost
 constexpr int kExpSlots = 3;
 
 template <int N>
@@ -487,9 +491,10 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
         const int part = 2 * wl + (head ? 1 : 0);
         const int out_row0 = (e0 + row0) * H + h;
         // The tile, with keys and values as they are (the usual case) or with powers of two of their own, 2^a of a key and 2^b of a value.  A key's comes into its
-        // score.  A value's goes with its probability, which is then measured against a maximum of its own: with z the score in log2 units, m the running
-        // maximum of z and w that of z + b,   sum = sum 2^(z - m),   O = sum 2^(z + b - w) V,   out = 2^(w - m) O / sum.   What a product with V is worth beside
-        // the others decides so how many bits its probability has, however far apart the sizes are; with b = 0 throughout every number is what it is without.
+        // score.  A value's goes with its probability, which is then measured against a maximum of its own: with z the score in log2 units against the
+        // row's reference m, and d the running maximum of z + b, rounded to an integer:   sum = sum 2^z,   O = sum 2^(z + b - d) V,   out = 2^d O / sum.  What
+        // a product with V is worth beside the others decides so how many bits its probability has, however far apart the sizes are; with b = 0 throughout d
+        // is 0, and every number is what it is without.
         auto walk = [&](auto scaled_c) __attribute__((always_inline)) {
             constexpr bool scaled = decltype(scaled_c)::value;
             constexpr int kVLoads = kRowLoads + scaled, kKVLoads = kLoads + 2 * scaled;
@@ -506,7 +511,7 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
             lds_barrier();
             f32x4 sc[2][RB], next[2][RB];  // scores of this step and of the one behind it
             float m[RB], l[RB];
-            float w[RB], sum_w[RB];              // (scaled) the maxima of z + b, sums of the probabilities that V is multiplied with
+            float d[RB];                         // (scaled)
             bool fresh = true, flushed = false;  // fresh: no maxima yet
             unsigned slot = 0;  // of step rel
             // the exponents of the keys or values 16 kb + 4 g4 .. + 3 of a step
@@ -514,21 +519,27 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
                 return *reinterpret_cast<__attribute__((address_space(3))) const u32x4*>(lds + at + 64 * kb + 16 * g4);
             };
             auto exponent = [](unsigned word) { return static_cast<int>(static_cast<signed char>(word)); };
+            // a score against the row's reference; moved: which has just moved
+            auto score = [&](int kb, int rb, int i, auto moved) __attribute__((always_inline)) {
+                const float z = fmaf(sc[kb][rb][i], c[rb], -m[rb]);
+                return decltype(moved)::value && z > kExpCap ? kExpCap : z;
+            };
             // a quarter of the probabilities of the scores of step rel, [rb][kb], and their sums
             f16x8 pr[RB];
             unsigned pw[RB][4];
             float sum[RB];
-            auto probabilities = [&](int kb, int rb) __attribute__((always_inline)) {
+            auto probabilities = [&](int kb, int rb, auto moved) __attribute__((always_inline)) {
                 float p[4];
                 u32x4 b = {0, 0, 0, 0};
                 if constexpr (scaled) b = exponents(slot + X::kVExp, kb);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    p[i] = __builtin_amdgcn_exp2f(fmaf(sc[kb][rb][i], c[rb], -m[rb]));
+                    const float z = score(kb, rb, i, moved);
+                    p[i] = __builtin_amdgcn_exp2f(z);
+                    if constexpr (scaled) p[i] = __uint_as_float(worked_out_here(__float_as_uint(p[i])));  // (here: scores are not kept for it)
                     sum[rb] += p[i];
                     if constexpr (scaled) {
-                        p[i] = __builtin_amdgcn_exp2f(fmaf(sc[kb][rb][i], c[rb], exponent(b[i]) - w[rb]));
-                        sum_w[rb] += p[i];
+                        p[i] = __builtin_amdgcn_exp2f(z + (exponent(b[i]) - d[rb]));
                     }
                 }
                 pw[rb][2 * kb] = worked_out_here(pack_f16x2(p[0], p[1]));  // (here, and not where it is used)
@@ -539,8 +550,10 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
             constexpr int kFrags = 2 * (KS + KSR), kAhead = 4;
             auto scores = [&](int rel1, unsigned slot1, auto with) __attribute__((always_inline)) {
                 constexpr bool probs = decltype(with)::value;
+                if constexpr (probs) {
 #pragma unroll
-                for (int rb = 0; rb < RB; ++rb) sum[rb] = sum_w[rb] = 0.f;
+                    for (int rb = 0; rb < RB; ++rb) sum[rb] = 0.f;
+                }
                 const int j0 = (k0 + rel1) * kExpStep;
                 u32x4 kf[kFrags];
                 auto read = [&](int f) __attribute__((always_inline)) {
@@ -573,7 +586,7 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
                     if (f + kAhead < kFrags) read(f + kAhead);
                     if constexpr (probs) {
                         constexpr int kEvery = kFrags / 4;
-                        if (f % kEvery == 0 && f / kEvery < 4) probabilities((f / kEvery) & 1, (f / kEvery) >> 1);
+                        if (f % kEvery == 0 && f / kEvery < 4) probabilities((f / kEvery) & 1, (f / kEvery) >> 1, std::false_type{});
                     }
                     in_this_order();
                 }
@@ -597,13 +610,13 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
                     for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[kb][rb][i]);
                 return mx * c[rb];
             };
-            auto largest_w = [&](int rb) __attribute__((always_inline)) {
+            auto largest_product = [&](int rb) __attribute__((always_inline)) {
                 float mx = -INFINITY;
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb) {
                     const u32x4 b = exponents(slot + X::kVExp, kb);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) mx = fmaxf(mx, fmaf(sc[kb][rb][i], c[rb], static_cast<float>(exponent(b[i]))));
+                    for (int i = 0; i < 4; ++i) mx = fmaxf(mx, score(kb, rb, i, std::true_type{}) + exponent(b[i]));
                 }
                 return mx;
             };
@@ -641,13 +654,14 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
             };
 
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb) m[rb] = l[rb] = w[rb] = 0.f;
+            for (int rb = 0; rb < RB; ++rb) m[rb] = l[rb] = d[rb] = 0.f;
             int rel = 0;
             f32x4 o[RB][NB];
             auto behind = [](unsigned x) { return x == 2 * X::kSlot ? 0u : x + X::kSlot; };
             scores(0, 0, std::false_type{});
             take_next();
-            bool grown = true;
+            bool grown = true, ready = false;  // ready: the probabilities of step rel are worked out
+            int settled = -1;                  // the last step whose scores moved a maximum
             while (true) {
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb)
@@ -655,12 +669,25 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
                     for (int cb = 0; cb < NB; ++cb) o[rb][cb] = f32x4{0.f, 0.f, 0.f, 0.f};
                 while (rel < steps && !grown) {
                     const unsigned slot1 = behind(slot), slot2 = behind(slot1);
-                    scores(rel + 1, slot1, std::true_type{});  // (behind the last step: of whatever lies there, not used)
-                    bool outgrown = false;
+                    // (behind the last step: of whatever lies there, not used)
+                    if (ready) {
+                        scores(rel + 1, slot1, std::false_type{});
+                        ready = false;
+                    } else {
+                        scores(rel + 1, slot1, std::true_type{});
+                        bool outgrown = false;
 #pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) outgrown |= sum[rb] > kExpMost || (scaled && sum_w[rb] > kExpMost);
-                    grown = __any(outgrown);
-                    if (grown) break;
+                        for (int rb = 0; rb < RB; ++rb) outgrown |= sum[rb] > kExpMost;
+                        if constexpr (scaled) {
+                            // (what V is multiplied with, as it stands: a half between kExpMost and infinity; a sum of it would cost a register in the loop)
+                            u16x2 least = {0xFFFF, 0xFFFF};
+#pragma unroll
+                            for (int i = 0; i < 4 * RB; ++i) least = __builtin_elementwise_min(least, __builtin_bit_cast(u16x2, pw[i / 4][i % 4]) - u16x2{kHalfMost, kHalfMost});
+                            outgrown |= min(least[0], least[1]) <= kHalfInfinity - kHalfMost;
+                        }
+                        grown = __any(outgrown);
+                        if (grown) break;
+                    }
 #pragma unroll
                     for (int rb = 0; rb < RB; ++rb) l[rb] += sum[rb];
                     if ((rel & 7) == 6) load_row_numbers((rel + 2) / 8 + 1);
@@ -681,14 +708,18 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
                     // new maxima, from the scores at hand; what has been summed up moves to memory, multiplied accordingly
 #pragma unroll
                     for (int rb = 0; rb < RB; ++rb) {
-                        const float mx = row_max(largest(rb));
+                        const float mx = moved_maximum(row_max(largest(rb)));
                         const float mn = fresh ? (mx == -INFINITY ? 0.f : mx) : fmaxf(mx, m[rb]);  // (a row that sees no key yet sees none at all)
                         const float a = fresh ? 0.f : __builtin_amdgcn_exp2f(m[rb] - mn);
-                        float a_w = a;  // of what V was multiplied with
+                        const float by = m[rb] - mn;
+                        m[rb] = mn;
+                        float a_v = a;  // for what V has been multiplied with
                         if constexpr (scaled) {
-                            const float mx_w = row_max(largest_w(rb)), wn = fresh ? (mx_w == -INFINITY ? 0.f : mx_w) : fmaxf(mx_w, w[rb]);
-                            a_w = __builtin_amdgcn_exp2f(w[rb] - wn);
-                            w[rb] = wn;
+                            float dn = rintf(row_max(largest_product(rb)));
+                            if (!fresh) dn = fmaxf(dn, rintf(d[rb] + by));
+                            if (dn == -INFINITY) dn = 0.f;
+                            a_v = __builtin_amdgcn_exp2f(d[rb] - dn + by);
+                            d[rb] = dn;
                         }
                         if (!fresh) {
                             float* const to = scratch(worked_out_here(lane)) + 16 * rb * N;
@@ -696,14 +727,23 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
                             for (int cb = 0; cb < NB; ++cb) {
                                 f32x4 y = o[rb][cb];
                                 if (flushed) y += *reinterpret_cast<const f32x4*>(to + 16 * cb);
-                                *reinterpret_cast<f32x4*>(to + 16 * cb) = y * a_w;
+                                *reinterpret_cast<f32x4*>(to + 16 * cb) = y * a_v;
                             }
                         }
                         l[rb] *= a;
-                        m[rb] = mn;
                     }
                     if (!fresh) flushed = true;
                     fresh = grown = false;
+                    ready = rel == settled;
+                    settled = rel;
+                    if (ready) [[unlikely]] {
+#pragma unroll
+                        for (int rb = 0; rb < RB; ++rb) {
+                            sum[rb] = 0.f;
+#pragma unroll
+                            for (int kb = 0; kb < 2; ++kb) probabilities(kb, rb, std::true_type{});
+                        }
+                    }
                 }
             }
 
@@ -723,7 +763,7 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
                     f32x4 y = o[rb][cb];
                     if (flushed) y += *reinterpret_cast<const f32x4*>(scratch(lane_now) + 16 * rb * N + 16 * cb);
                     y *= inv;
-                    if constexpr (scaled) y *= __builtin_amdgcn_exp2f(w[rb] - m[rb]);
+                    if constexpr (scaled) y *= __builtin_amdgcn_exp2f(d[rb]);
                     const int col = 16 * cb + 4 * g4;
                     if (odd_seen) {
                         // (a weight is positive: an infinity stays one, two of opposite sign and NaN give NaN; the keys of the steps they were taken out of)

@@ -195,6 +195,15 @@ __device__ __forceinline__ bool latent_share(const LatentBatch& b, const LatentS
     return true;
 }
 
+// What scores are measured against, from the largest of them (both in log2 units).  A probability is 2^(c s - m) out of one fused multiply-add, but m itself is
+// rounded to 32 bits: from 2^22 on by so much that it shows, from 2^28 on by so much that the largest score's own probability would be 2^16 or 2^-16 and beyond.
+// Such a maximum is taken a few steps lower than it is, so that no row's largest probabilities vanish, and what they are too large by, its user holds
+// to a limit; scores that fp32 cannot tell apart then weigh the same.
+__device__ __forceinline__ float moved_maximum(float largest) {
+    const float a = fabsf(largest);
+    return a >= 4194304.f && a < INFINITY ? largest - a * 2.384185791015625e-7f : largest;
+}
+
 // Partial results: slot 2 w holds what workgroup w did of a tile that it did not begin, slot 2 w + 1 of one that it began and did not finish.
 // Slots 2 n .. 3 n - 1 are the workgroups' scratch memory.  Records of a slot: {first row of the output, rows, kPartHead | kPartLast, rows of the output from one to the next}; flags 0: nothing.
 constexpr int kPartHead = 1, kPartLast = 2;

@@ -90,3 +90,54 @@ def test_expanded_rows_of_no_request_may_hold_anything(pa, gpu_device, kind, val
     got = torch.cat([out[2:5], out[6:10]])
     check(got, ref, bound, f"{value}, {kind}")
     assert torch.equal(bits(got), bits(alone)) and bool((out[[0, 1, 5, 10, 16]] == 9.0).all())
+
+
+# ---- scores --------------------------------------------------------------------------------------------------------------------
+
+def check_winners(b, out, form):
+    """Scores so large that one key has all the weight: its value comes out.  Which key it is may be left to rounding only where two scores are nearer to
+    one another than fp32 sums of their magnitude are exact, (width + 2) 2^-24 times the sum of the products' magnitudes, for each of the two, and e^-30."""
+    rows, t, told_apart = b.stored(), 0, 0
+    h, h16 = HALF[b.dtype], 0.0 if b.dtype == torch.float32 else HALF[torch.float16]
+    for r, (n, e) in enumerate(zip(b.prefix, b.ext)):
+        keys = torch.cat([rows[b.slots[r].to(rows.device)], b.c[t:t + e].double()])
+        q, lat, rope = b.q[t:t + e].double(), keys[:, :b.R], keys[:, b.R:]
+        hidden = torch.arange(n + e, device=q.device)[None] > n + torch.arange(e, device=q.device)[:, None]
+        for x in range(b.H):
+            if form == "absorbed":
+                k, v, size = keys, lat, (b.R + P + 2) * 2.0 ** -24 * (q[:, x].abs() @ keys.abs().T)
+                tol_v = v.abs() * h
+            else:
+                wk, wv = b.w_k[x].double(), b.w_v[x].double()
+                k, v = torch.cat([lat @ wk.T, rope], 1), lat @ wv.T
+                sums = (b.R + 2) * 2.0 ** -24 + (b.N + 2) * 2.0 ** -24 * (b.dtype == torch.float32)
+                grow = torch.cat([lat.abs() @ wk.abs().T * sums + k[:, :b.N].abs() * h16 + 2.0 ** -17 * h16 / HALF[torch.float16] * k[:, :b.N].abs().amax(1, True), rope * 0], 1)
+                size = (b.N + P + 2) * 2.0 ** -24 * (q[:, x].abs() @ k.abs().T) + q[:, x].abs() @ grow.T
+                tol_v = v.abs() * (h + h16) * 1.01 + 2.0 ** -17 * v.abs().amax(1, True) * (h16 > 0) + lat.abs() @ wv.abs().T * sums
+            z = (q[:, x] @ k.T).masked_fill(hidden, -torch.inf)
+            best = z.amax(1, keepdim=True)
+            off = (size.masked_fill(hidden, 0)).amax(1, keepdim=True)
+            rival = (z + 2 * off + 30 / b.scale >= best) & ~hidden
+            alone = rival.sum(1) == 1
+            told_apart += int(alone.sum())
+            got = out[t:t + e, x].double()
+            win = z.argmax(1)
+            assert bool(((got - v[win]).abs() <= tol_v[win] + h * v[win].abs())[alone].all()), (r, x)
+            low = torch.where(rival[..., None], v - tol_v, torch.inf).amin(1)       # beside rivals: between their values
+            high = torch.where(rival[..., None], v + tol_v, -torch.inf).amax(1)
+            room = 2 * h * torch.maximum(low.abs(), high.abs())
+            assert bool(((got >= low - room) & (got <= high + room)).all()), (r, x)
+        t += e
+    return told_apart
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("of_q,of_c", [(12, 10), (14, 12), (15, 13), (20, 10), (17, 16), (22, 18), (40, 20)])
+@pytest.mark.parametrize("prefix,ext", [([400, 33], [3, 40]), ([3000], [5])])
+def test_expanded_scores_beyond_the_steps_of_fp32(pa, gpu_device, kind, of_q, of_c, prefix, ext):
+    """Scores of 2^22 to 2^60."""
+    b = Batch(gpu_device, prefix, ext, 3, 512, *KINDS[kind], seed=12).weights(128)
+    b.rows_pool, b.c, b.q = b.rows_pool * 2.0 ** of_c, b.c * 2.0 ** of_c, b.q * 2.0 ** of_q
+    b.fill(pa)
+    apart = check_winners(b, b.expanded(pa), "expanded")
+    assert apart >= b.T * b.H // 2
