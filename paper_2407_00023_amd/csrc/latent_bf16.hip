@@ -19,7 +19,8 @@
 // products the probabilities of step i + 1.  Rows are loaded straight into LDS, two steps ahead of the output (M = 128) or three, their loads set out beside the first
 // products of the scores.  The running maximum of a row moves only when a lane's probabilities of a step sum to more than kMost: the wave that sees it sets a
 // flag, which all waves find in the next interval, and they settle on new maxima together (settle()), the scores computed once more; until then a
-// probability may be as large as kMost, which fp32 and bf16 hold as exactly as 1.
+// probability may be as large as kMost, which fp32 and bf16 hold as exactly as 1.  Against maxima so large that their rounding shows (moved_maximum()) those of the
+// settlement itself are held to 2^kCap; the step counts as done then.
 //
 // Measured: 64 heads, 16 requests of 20 to 80 new tokens over 4 documents of 16 384 rows (1.9 TFLOP): 1850 us, 1.05 PFLOP/s, where a plain product of 16 384
 // squared reaches 1.39; bound by LDS and by waiting beside the matrix cores, which are busy 45 % of the cycles.  128 heads, 128 requests of one token, 500 to 7800 keys: 257 us.
@@ -59,6 +60,7 @@ __device__ __forceinline__ void products_done() { asm volatile("s_nop 15\n\ts_no
 
 constexpr int kStep = 32;       // keys of a step
 constexpr float kMost = 1099511627776.f;  // 2^40
+constexpr float kCap = 36.f;    // log2 of a probability against a maximum that has just moved, at most: eight of them are less than kMost
 
 __device__ const uint4 g_zero_row[128] = {};  // stands for keys behind the last one of a tile
 
@@ -371,11 +373,12 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
         };
         // a piece of the probabilities of the scores against the maxima as they stand, into buffer rel % 2; their sums
         float sum[RW];
-        auto probabilities = [&](int rel, int kb, int rb) __attribute__((always_inline)) {
+        auto probabilities = [&](int rel, int kb, int rb, auto moved) __attribute__((always_inline)) {
             float p[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                p[i] = __builtin_amdgcn_exp2f(fmaf(sc[kb][rb][i], scale_log2e, -m[rb]));
+                const float z = fmaf(sc[kb][rb][i], scale_log2e, -m[rb]);
+                p[i] = __builtin_amdgcn_exp2f(decltype(moved)::value && z > kCap ? kCap : z);
                 sum[rb] += p[i];
             }
             *reinterpret_cast<__attribute__((address_space(3))) u32x2*>(lds + ((p_wr + (rel & 1) * X::kProb + rb * 1024) ^ (kb * 32))) =
@@ -394,7 +397,7 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
         auto settle = [&](int rel, bool first, auto flush) {
 #pragma unroll
             for (int rb = 0; rb < RW; ++rb) {
-                const float mx = row_max(largest(rb));
+                const float mx = moved_maximum(row_max(largest(rb)));
                 if (g4 == 0) s_red[kgroup * M + wrow + 16 * rb + n] = mx;
             }
             lds_barrier();
@@ -419,7 +422,7 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
 #pragma unroll
             for (int rb = 0; rb < RW; ++rb)
 #pragma unroll
-                for (int kb = 0; kb < KW; ++kb) probabilities(rel, kb, rb);
+                for (int kb = 0; kb < KW; ++kb) probabilities(rel, kb, rb, std::true_type{});
             lds_barrier();
         };
         // Output of step rel, and beside it the probabilities of the scores at hand, of step rel + 1.
@@ -456,7 +459,7 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
                     if (RB * NB == 64 && rb == RB - 1 && cb >= NB - kInVector) mfma_next_done(o[rb][cb], v, pf[rb]);
                     else o[rb][cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf[rb], o[rb][cb], 0, 0, 0);
                 }
-                if (cb % kEvery == 0) probabilities(rel + 1, (cb / kEvery) % KW, (cb / kEvery) / KW);
+                if (cb % kEvery == 0) probabilities(rel + 1, (cb / kEvery) % KW, (cb / kEvery) / KW, std::false_type{});
                 in_this_order();
             }
         };

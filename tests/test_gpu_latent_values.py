@@ -141,3 +141,18 @@ def test_expanded_scores_beyond_the_steps_of_fp32(pa, gpu_device, kind, of_q, of
     b.fill(pa)
     apart = check_winners(b, b.expanded(pa), "expanded")
     assert apart >= b.T * b.H // 2
+
+
+KINDS_TOLD = [("f32", 0)] + [(k, x) for k in ("bf16", "bf16_kv8") for x in TOLD]   # (fp32 has no tiles)
+
+
+@pytest.mark.parametrize("kind,told", KINDS_TOLD, indirect=["told"])
+@pytest.mark.parametrize("R", [512, 256])
+@pytest.mark.parametrize("H", [3, 64])
+@pytest.mark.parametrize("of_q,of_c", [(12, 10), (16, 16), (18, 15), (22, 18), (60, 20)])
+def test_absorbed_scores_beyond_the_steps_of_fp32(pa, gpu_device, kind, R, H, of_q, of_c, told):
+    b = Batch(gpu_device, [400, 33, 1500], [3, 40 if H == 3 else 2, 1], H, R, *KINDS[kind], seed=13)
+    b.rows_pool, b.c, b.q = b.rows_pool * 2.0 ** of_c, b.c * 2.0 ** of_c, b.q * 2.0 ** of_q
+    b.fill(pa)
+    apart = check_winners(b, b.absorbed(pa), "absorbed")
+    assert apart >= b.T * b.H // 2
