@@ -446,28 +446,36 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
         };
 
         // ---- the wave's rows of Q, times a power of two that brings the largest of a row to [2^8, 2^9) ----
+        // (A head with keys of powers of their own: what meets them by itself, its power relative to the row's goes with theirs.  Small ones would be out of
+        // fp16's range beside rotary values otherwise, and decide for large keys all the same.)
         load_row_numbers(0);
         f16x8 q[RB][KS];
         bf16x8 qr[RB][KSR];
         float c[RB];
+        int q_exp[RB];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
             const int row = min(wrow + 16 * rb + n, rows_here - 1);  // (rows behind the last repeat it)
             const uint4* const src = reinterpret_cast<const uint4*>(q_ext + (static_cast<int64_t>(e0 + row0 + row) * H + h) * QW);
             uint4 raw[KS + KSR];
-            unsigned top = 0;
+            unsigned top = 0, top_n = 0;
 #pragma unroll
             for (int s = 0; s < KS + KSR; ++s) {
+                if (s == KS) top_n = top;
                 raw[s] = src[4 * s + g4];
                 const unsigned w[4] = {raw[s].x, raw[s].y, raw[s].z, raw[s].w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) top = max(top, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
             }
-            top = max(top, static_cast<unsigned>(__shfl_xor(static_cast<int>(top), 16)));
-            top = max(top, static_cast<unsigned>(__shfl_xor(static_cast<int>(top), 32)));
-            const int e = static_cast<int>(top >> 7);
-            const int k = e == 0 || e == 255 ? 0 : max(min(e - 127 - 8, 126), -126);
-            const float by = power_of_two(-k);
+            auto exponent_of = [](unsigned t) {
+                t = max(t, static_cast<unsigned>(__shfl_xor(static_cast<int>(t), 16)));
+                t = max(t, static_cast<unsigned>(__shfl_xor(static_cast<int>(t), 32)));
+                const int e = static_cast<int>(t >> 7);
+                return e == 0 || e == 255 ? 0 : max(min(e - 127 - 8, 126), -126);
+            };
+            const int k = exponent_of(top), alone = min(exponent_of(top_n), k), k_n = is_scaled ? alone : k;
+            const float by = power_of_two(-k), by_n = power_of_two(-k_n);
+            q_exp[rb] = k_n - k;
             c[rb] = scale_log2e * power_of_two(k);
 #pragma unroll
             for (int s = 0; s < KS + KSR; ++s) {
@@ -475,7 +483,7 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
                 unsigned y[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float lo = __uint_as_float(w[i] << 16) * by, hi = __uint_as_float(w[i] & 0xFFFF0000u) * by;
+                    const float times = s < KS ? by_n : by, lo = __uint_as_float(w[i] << 16) * times, hi = __uint_as_float(w[i] & 0xFFFF0000u) * times;
                     y[i] = s < KS ? pack_f16x2(lo, hi) : pack_bf16x2(lo, hi);
                 }
                 const uint4 z = make_uint4(y[0], y[1], y[2], y[3]);
@@ -574,7 +582,7 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
 #pragma unroll
                             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                                for (int rb = 0; rb < RB; ++rb) next[y][rb][i] *= power_of_two(exponent(a[i]));
+                                for (int rb = 0; rb < RB; ++rb) next[y][rb][i] *= power_of_two(max(exponent(a[i]) + q_exp[rb], -126));
                         }
                     }
 #pragma unroll

@@ -40,7 +40,7 @@ def test_expanded_values_some_of_which_are_small(pa, gpu_device, kind, prefix, e
 
 
 @pytest.mark.parametrize("kind", ["bf16", "bf16_kv8"])
-@pytest.mark.parametrize("of", [-20, -14, -12, -10, -9, -8, 8, 14])
+@pytest.mark.parametrize("of", [-20, -14, -12, -10, -9, -8, 8, 14, 30, 60])
 @pytest.mark.parametrize("prefix,ext", [([1024, 1024], [3, 5]), ([100, 33], [40, 200])])
 def test_expanded_requests_whose_rows_differ_in_size(pa, gpu_device, kind, of, prefix, ext):
     """The latent parts of request 1 are 2^of times those of request 0: each is held to what it would be by itself, and a call repeats its bits."""
