@@ -441,9 +441,10 @@ size_t pa_latent_expanded_workspace_bytes(int B, int64_t T, int64_t max_kv_len, 
  * Less arithmetic than the absorbed form from some hundred new tokens behind a cached one on: a row of
  * q costs 2 (2 N + P) operations per key and head instead of 2 (2 R + P), against 4 N R once per
  * distinct cached slot and head.  bf16: keys and values are held to 11 bits, or to 2^-17 of the
- * largest of their token and head where that is more, whatever else is in the batch.  The other
- * arguments as above; max_kv_len binds here with bf16: of a batch in which a request with extend
- * tokens has more keys nothing is computed, and pa_extend_status says so. */
+ * largest of their token and head where that is more, whatever else is in the batch; probabilities
+ * to 11 bits, or to 2^-33 of their row's largest (times its value's power of two, where values are out
+ * of [2^-8, 2^15)).  The other arguments as above; max_kv_len binds here with bf16: of a batch in which
+ * a request with extend tokens has more keys nothing is computed, and pa_extend_status says so. */
 int pa_latent_attention_expanded(const void* q_ext, const void* c_ext, const void* w_k, const void* w_v,
                                  const void* latent_pool, const int32_t* slot_idx, const int32_t* slot_offsets,
                                  const int32_t* prefix_len, const int32_t* ext_len, const int32_t* ext_offsets,

@@ -319,9 +319,13 @@ __device__ __forceinline__ int swz_v(int row) {
 // the loop, what it has summed up goes to memory, multiplied accordingly, and the accumulators begin anew (inside the loop the compiler
 // would keep a second copy of them).  A maximum so large that its rounding shows (moved_maximum()) does not help the step it was taken from: if a step makes the
 // wave leave the loop a second time, its probabilities are worked out there, held to 2^kExpCap, and the loop goes on whatever they sum to.
-constexpr float kExpMost = 16384.f;  // 2^14 is a large fp16 still
-constexpr unsigned short kHalfMost = 0x7400, kHalfInfinity = 0x7C00;  // kExpMost and infinity in fp16
-constexpr float kExpCap = 11.f;      // log2 of what probabilities are held to then: eight of them are kExpMost
+// A settled maximum stands for a probability of 2^kExpBits: fp16 holds what is as far below it as 2^-22 in 11 bits then, and what is lost is
+// 2^-33 of it.  (With 1 for the maximum these are 2^-14 and 2^-25: many keys of little weight each, behind one that has nearly all of it and a small value, lost
+// a fortieth at 2^-22.6, a fifth at 2^-26.)
+constexpr float kExpBits = 8.f;
+constexpr float kExpMost = 32768.f;  // 2^15 is the last power of two that fp16 holds
+constexpr unsigned short kHalfMost = 0x7800, kHalfInfinity = 0x7C00;  // kExpMost and infinity in fp16
+constexpr float kExpCap = 12.f;      // log2 of what probabilities are held to then: eight of them are kExpMost
 constexpr int kExpSlots = 3;
 
 template <int N>
@@ -500,7 +504,7 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
         const int out_row0 = (e0 + row0) * H + h;
         // The tile, with keys and values as they are (the usual case) or with powers of two of their own, 2^a of a key and 2^b of a value.  A key's comes into its
         // score.  A value's goes with its probability, which is then measured against a maximum of its own: with z the score in log2 units against the
-        // row's reference m, and d the running maximum of z + b, rounded to an integer:   sum = sum 2^z,   O = sum 2^(z + b - d) V,   out = 2^d O / sum.  What
+        // row's reference m, and d the running maximum of z + b, rounded to an integer, less kExpBits:   sum = sum 2^z,   O = sum 2^(z + b - d) V,   out = 2^d O / sum.  What
         // a product with V is worth beside the others decides so how many bits its probability has, however far apart the sizes are; with b = 0 throughout d
         // is 0, and every number is what it is without.
         auto walk = [&](auto scaled_c) __attribute__((always_inline)) {
@@ -716,14 +720,14 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
                     // new maxima, from the scores at hand; what has been summed up moves to memory, multiplied accordingly
 #pragma unroll
                     for (int rb = 0; rb < RB; ++rb) {
-                        const float mx = moved_maximum(row_max(largest(rb)));
+                        const float mx = moved_maximum(row_max(largest(rb))) - kExpBits;
                         const float mn = fresh ? (mx == -INFINITY ? 0.f : mx) : fmaxf(mx, m[rb]);  // (a row that sees no key yet sees none at all)
                         const float a = fresh ? 0.f : __builtin_amdgcn_exp2f(m[rb] - mn);
                         const float by = m[rb] - mn;
                         m[rb] = mn;
                         float a_v = a;  // for what V has been multiplied with
                         if constexpr (scaled) {
-                            float dn = rintf(row_max(largest_product(rb)));
+                            float dn = rintf(row_max(largest_product(rb))) - kExpBits;
                             if (!fresh) dn = fmaxf(dn, rintf(d[rb] + by));
                             if (dn == -INFINITY) dn = 0.f;
                             a_v = __builtin_amdgcn_exp2f(d[rb] - dn + by);

@@ -156,3 +156,51 @@ def test_absorbed_scores_beyond_the_steps_of_fp32(pa, gpu_device, kind, R, H, of
     b.fill(pa)
     apart = check_winners(b, b.absorbed(pa), "absorbed")
     assert apart >= b.T * b.H // 2
+
+
+def weights_far_below(b):
+    """The expanded form's definition and a bound that knows of the probabilities' fp16 only that they are off by 2^-11 of themselves or by 2^-33 of their row's
+    largest, whichever is more.  The queries have no latent part here: scores are products of rotary parts, as given."""
+    h, outs, bounds, t = HALF[b.dtype], [], [], 0
+    h16, rows = 0.0 if b.dtype == torch.float32 else HALF[torch.float16], b.stored()
+    for r, (n, e) in enumerate(zip(b.prefix, b.ext)):
+        keys = torch.cat([rows[b.slots[r].to(rows.device)], b.c[t:t + e].double()])
+        lat, q_r = keys[:, :b.R], b.q[t:t + e, :, b.N:].double()
+        assert not bool(b.q[t:t + e, :, :b.N].any())
+        hidden = torch.arange(n + e, device=keys.device)[None] > n + torch.arange(e, device=keys.device)[:, None]
+        for x in range(b.H):
+            v, size_v = lat @ b.w_v[x].double().T, lat.abs() @ b.w_v[x].double().abs().T
+            z = (q_r[:, x] @ keys[:, b.R:].T * b.scale).masked_fill(hidden, -torch.inf)
+            p = torch.softmax(z, 1)
+            out = p @ v
+            dz = ((P + 2) * 2.0 ** -24 * (q_r[:, x].abs() @ keys[:, b.R:].abs().T) * b.scale).masked_fill(hidden, 0).amax(1, keepdim=True)
+            grow_v = size_v * (b.R + 2) * 2.0 ** -24 + (h16 * v.abs() + (2.0 ** -17 if h16 else 0.0) * v.abs().amax(1, keepdim=True))
+            bound = (p @ v.abs()) * (2 * dz + 2.0 ** -20 + (n + e + 64) * 2.0 ** -24 + h16) + h * out.abs() + p @ grow_v * (1 + h) + 1e-30
+            if h16:
+                bound = bound + 2.0 ** -33 * p.amax(1, keepdim=True) * ((~hidden).double() @ v.abs())
+            outs.append(out)
+            bounds.append(bound)
+        t += e
+    lay = lambda ys: torch.cat([torch.stack(ys[r * b.H:(r + 1) * b.H], 1) for r in range(len(b.prefix))])
+    return lay(outs), lay(bounds)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("far", [6, 14, 17.3, 19.3, 20.4, 22.6, 24.5, 26])
+@pytest.mark.parametrize("where", ["first", "last"])
+def test_expanded_many_keys_far_below_the_largest(pa, gpu_device, kind, far, where):
+    """A key takes nearly all the weight and has a value of zero; what comes out are the many others, 2^-far of it each."""
+    prefix, ext, H = [3000, 700], [3, 40], 2
+    b = Batch(gpu_device, prefix, ext, H, 512, *KINDS[kind], seed=14).weights(128)
+    g = torch.Generator().manual_seed(15)
+    row = torch.randn(1, 512, generator=g)
+    b.rows_pool = torch.cat([row + 0.05 * torch.randn(b.num_slots, 512, generator=g), torch.zeros(b.num_slots, P)], 1).to(b.dtype).to(gpu_device)
+    b.c = torch.cat([row + 0.05 * torch.randn(b.T, 512, generator=g), torch.zeros(b.T, P)], 1).to(b.dtype).to(gpu_device)
+    b.q = torch.zeros_like(b.q)
+    b.q[..., b.N] = 8
+    for s in b.slots:
+        at = s[0] if where == "first" else s[-1]
+        b.rows_pool[at] = 0
+        b.rows_pool[at, 512] = far * 0.6931471805599453 / (8 * b.scale)
+    b.fill(pa)
+    check(b.expanded(pa), *weights_far_below(b), f"2^-{far}, {kind}")
