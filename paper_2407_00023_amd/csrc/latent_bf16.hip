@@ -297,7 +297,7 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
 
         // ---- the pieces of an interval ----
         // Keys that some row of the tile does not see may hold an infinity or NaN, and 0 times that is NaN: before the output of a step with such keys, when
-        // its scores are done, the wave that loaded a row takes such values out of it; the end of the tile gives them to the rows that see them.
+        // its scores are done, the wave that loaded a row takes such values out of it; the end of the tile makes the column NaN for the rows that see them.
         auto has_hidden = [&](int rel) { return vis_min < key_end && (k0 + rel + 1) * kStep > vis_min; };
         auto clean = [&](int lat_slot) {
             const unsigned at_row = lat_slot * X::kLat + 8 * wave * X::kLatRow + 16 * worked_out_here(lane);
@@ -594,14 +594,14 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
                 x *= inv;
                 const int col = 16 * (NB * wave + cb) + 4 * g4;
                 if (odd_seen) {
-                    // (a weight is positive: an infinity stays one, two of opposite sign and NaN give NaN)
+                    // (The key's own score is then infinite or NaN too: its weight is NaN, or 0, and 0 times an infinity is NaN.)
                     for (int j = max(vis_min & ~(kStep - 1), k0 * kStep); j < min(sees, k1 * kStep); ++j) {
                         const bool cached = j < P;
                         if (KV8 && cached) continue;  // (the 8-bit pool holds neither)
                         const auto* const c4 = reinterpret_cast<const unsigned short*>(row_address(j, cached ? slots[j] : 0)) + col;
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            if ((c4[i] & 0x7F80) == 0x7F80) x[i] += __uint_as_float(static_cast<unsigned>(c4[i]) << 16);
+                            if ((c4[i] & 0x7F80) == 0x7F80) x[i] = NAN;
                     }
                 }
                 if (whole)

@@ -427,7 +427,7 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
         };
 
         // Steps with keys that some row of the tile does not see, or behind the last: 0 times an infinity or NaN of such a key would be NaN.  The wave
-        // that loaded a row of V takes such values out of it, and the end of the tile gives them to the rows that see them.
+        // that loaded a row of V takes such values out of it, and the end of the tile makes the column NaN for the rows that see them.
         auto clean = [&](int rel, unsigned slot) __attribute__((always_inline)) {
             if ((k0 + rel + 1) * kExpStep <= P + row0 + 1) return;
             const unsigned at_v = slot + X::kK + 8 * wave * X::kRow + 16 * lane;
@@ -778,13 +778,14 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
                     if constexpr (scaled) y *= __builtin_amdgcn_exp2f(d[rb]);
                     const int col = 16 * cb + 4 * g4;
                     if (odd_seen) {
-                        // (a weight is positive: an infinity stays one, two of opposite sign and NaN give NaN; the keys of the steps they were taken out of)
+                        // (A latent value that is not finite makes the key so too, and its score: the weight is NaN, or 0, and 0 times an infinity is NaN.  The keys
+                        // of the steps they were taken out of.)
                         for (int j = max((P + row0 + 1) & ~(kExpStep - 1), k0 * kExpStep); j < min(P + row0 + row + 1, k1 * kExpStep); ++j) {
                             const int64_t at_row = row_of[j];
                             const unsigned short* const v4 = reinterpret_cast<const unsigned short*>(v_rows) + at_row * N + col;
 #pragma unroll
                             for (int i = 0; i < 4; ++i)
-                                if ((v4[i] & 0x7C00) == 0x7C00) y[i] += (v4[i] & 0x3FF) ? NAN : (v4[i] & 0x8000) ? -INFINITY : INFINITY;
+                                if ((v4[i] & 0x7C00) == 0x7C00) y[i] = NAN;
                         }
                     }
                     if (whole)

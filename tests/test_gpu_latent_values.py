@@ -204,3 +204,94 @@ def test_expanded_many_keys_far_below_the_largest(pa, gpu_device, kind, far, whe
         b.rows_pool[at, 512] = far * 0.6931471805599453 / (8 * b.scale)
     b.fill(pa)
     check(b.expanded(pa), *weights_far_below(b), f"2^-{far}, {kind}")
+
+
+# ---- infinities ----------------------------------------------------------------------------------------------------------------
+
+def definition_with_infinities(b, form):
+    """The definition row by row over the keys that the row sees, as arithmetic has it: a score of +infinity or NaN makes the row NaN, one of -infinity gives its
+    key the weight 0, and 0 times an infinite value is NaN in its column.  The bound (elsewhere) is that of Batch.reference over the keys that have a weight."""
+    h, rows, t = HALF[b.dtype], b.stored(), 0
+    h16 = HALF[torch.float16] if form == "expanded" and b.dtype != torch.float32 else 0.0
+    ref = torch.full((b.T, b.H, b.R if form == "absorbed" else b.N), torch.nan, dtype=torch.float64, device=rows.device)
+    bound = torch.ones_like(ref)
+    for r, (n, e) in enumerate(zip(b.prefix, b.ext)):
+        keys = torch.cat([rows[b.slots[r].to(rows.device)], b.c[t:t + e].double()])
+        lat, rope = keys[:, :b.R], keys[:, b.R:]
+        for x in range(b.H):
+            if form == "absorbed":
+                k, v, grow_k, grow_v = keys, lat, torch.zeros_like(keys), torch.zeros_like(lat)
+            else:
+                wk, wv = b.w_k[x].double(), b.w_v[x].double()
+                k, v = torch.cat([lat @ wk.T, rope], 1), lat @ wv.T
+                sums = (b.R + b.N + 2) * 2.0 ** -24
+                grow_k = torch.cat([lat.abs() @ wk.abs().T * sums + h16 * k[:, :b.N].abs() + (2.0 ** -17 * k[:, :b.N].abs().amax(1, True) if h16 else 0.0), rope * 0], 1)
+                grow_v = lat.abs() @ wv.abs().T * sums + h16 * v.abs() + (2.0 ** -17 * v.abs().amax(1, True) if h16 else 0.0)
+            for i in range(e):
+                seen, q = n + i + 1, b.q[t + i, x].double()
+                z = (k[:seen] * q).sum(1) * b.scale
+                if bool(torch.isnan(z).any()) or bool((z == torch.inf).any()) or not bool(torch.isfinite(z).any()):
+                    continue
+                keep = torch.isfinite(z)
+                p, vk = torch.softmax(z[keep], 0), v[:seen][keep]
+                out = p @ vk
+                dz = float((((k.shape[1] + 2) * 2.0 ** -24 * k[:seen][keep].abs() + grow_k[:seen][keep]) @ q.abs()).max()) * b.scale
+                hp = 0.0 if b.dtype == torch.float32 else h16 or h
+                bound[t + i, x] = (p @ vk.abs()) * (2 * dz + 2.0 ** -20 + (seen + 64) * 2.0 ** -24 + hp) + h * out.abs() + p @ grow_v[:seen][keep] * (1 + h) + 1e-30
+                if h16:
+                    bound[t + i, x] += 2.0 ** -33 * vk.abs().sum(0)
+                ref[t + i, x] = torch.where(torch.isfinite(v[:seen]).all(0), out, torch.nan)
+        t += e
+    return ref, bound
+
+
+def check_with_infinities(out, ref, bound, what=""):
+    assert torch.equal(torch.isnan(out), torch.isnan(ref)), (what, int(torch.isnan(out).sum()), int(torch.isnan(ref).sum()))
+    there = ~torch.isnan(ref)
+    check(out[there], ref[there], bound[there], what)
+
+
+FORMS_KINDS_TOLD = [("absorbed",) + x for x in KINDS_TOLD] + [("expanded", k, 0) for k in KINDS]
+
+
+def looking_away(b, form, where, value):
+    """Queries of heads 0, 4, 8, ... whose score with a latent `value` at column `where` is -infinity, those of 1, 5, ... +infinity, 2, 6, ... NaN;
+    3, 7, ... as they are."""
+    s = 1.0 if value > 0 else -1.0
+    for x in range(b.H):
+        if x % 4 == 3:
+            continue
+        if form == "absorbed":
+            b.q[:, x, where] = [-s, s, 0][x % 4]
+        else:
+            at = torch.sign(b.w_k[x, :, where].float())
+            b.q[:, x, :b.N] = ((-s if x % 4 == 0 else s) * at * b.q[:, x, :b.N].float().abs().clamp(min=0.01)).to(b.dtype)
+            if x % 4 == 2:
+                b.q[:, x, 0] = 0
+
+
+@pytest.mark.parametrize("form,kind,told", FORMS_KINDS_TOLD, indirect=["told"])
+@pytest.mark.parametrize("value", [float("inf"), -float("inf")])
+@pytest.mark.parametrize("prefix,ext,row", [([45, 10], [40, 3], 21), ([2000], [4], 1), ([3, 64], [2, 1], 1)])
+def test_infinite_latent_values_in_new_rows(pa, gpu_device, form, kind, value, prefix, ext, row, told):
+    b = Batch(gpu_device, prefix, ext, 8, 512, *KINDS[kind], seed=16).fill(pa)
+    if form == "expanded":
+        b.weights(128)
+    looking_away(b, form, 300, value)
+    b.c[row, 300] = value
+    out = (b.absorbed if form == "absorbed" else b.expanded)(pa)
+    check_with_infinities(out, *definition_with_infinities(b, form), f"{value} in row {row}, {kind}")
+
+
+@pytest.mark.parametrize("form,kind,told", [x for x in FORMS_KINDS_TOLD if x[1] != "bf16_kv8"], indirect=["told"])
+@pytest.mark.parametrize("value", [float("inf"), -float("inf")])
+@pytest.mark.parametrize("at", [0, 500, 1998, 1999])
+def test_infinite_latent_values_in_cached_rows(pa, gpu_device, form, kind, value, at, told):
+    b = Batch(gpu_device, [2000, 90], [3, 2], 8, 512, *KINDS[kind], seed=17)
+    b.rows_pool[b.slots[0][at], 300] = value
+    b.fill(pa)
+    if form == "expanded":
+        b.weights(128)
+    looking_away(b, form, 300, value)
+    out = (b.absorbed if form == "absorbed" else b.expanded)(pa)
+    check_with_infinities(out, *definition_with_infinities(b, form), f"{value} in key {at}, {kind}")
