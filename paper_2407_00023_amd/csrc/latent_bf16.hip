@@ -405,7 +405,7 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
             auto new_max = [&](int row) {
                 float x = s_red[row];
                 if (KG == 2) x = fmaxf(x, s_red[M + row]);
-                if (first) return x == -INFINITY ? 0.f : x;  // (a row that sees no key here sees none behind it either)
+                if (first) return x == -INFINITY ? kNoMaximum : x;
                 return fmaxf(x, s_max[row]);
             };
             if (!first) flush([&](int row) { return __builtin_amdgcn_exp2f(s_max[row] - new_max(row)); });

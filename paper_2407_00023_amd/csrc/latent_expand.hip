@@ -721,7 +721,7 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
 #pragma unroll
                     for (int rb = 0; rb < RB; ++rb) {
                         const float mx = moved_maximum(row_max(largest(rb))) - kExpBits;
-                        const float mn = fresh ? (mx == -INFINITY ? 0.f : mx) : fmaxf(mx, m[rb]);  // (a row that sees no key yet sees none at all)
+                        const float mn = fresh ? (mx == -INFINITY ? kNoMaximum : mx) : fmaxf(mx, m[rb]);
                         const float a = fresh ? 0.f : __builtin_amdgcn_exp2f(m[rb] - mn);
                         const float by = m[rb] - mn;
                         m[rb] = mn;

@@ -204,6 +204,9 @@ __device__ __forceinline__ float moved_maximum(float largest) {
     return a >= 4194304.f && a < INFINITY ? largest - a * 2.384185791015625e-7f : largest;
 }
 
+// ... of a row that has met no score but -infinity: the next one outgrows it, however small
+constexpr float kNoMaximum = -3.4028234663852886e38f;
+
 // Partial results: slot 2 w holds what workgroup w did of a tile that it did not begin, slot 2 w + 1 of one that it began and did not finish.
 // Slots 2 n .. 3 n - 1 are the workgroups' scratch memory.  Records of a slot: {first row of the output, rows, kPartHead | kPartLast, rows of the output from one to the next}; flags 0: nothing.
 constexpr int kPartHead = 1, kPartLast = 2;

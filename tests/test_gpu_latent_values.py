@@ -295,3 +295,27 @@ def test_infinite_latent_values_in_cached_rows(pa, gpu_device, form, kind, value
     looking_away(b, form, 300, value)
     out = (b.absorbed if form == "absorbed" else b.expanded)(pa)
     check_with_infinities(out, *definition_with_infinities(b, form), f"{value} in key {at}, {kind}")
+
+
+@pytest.mark.parametrize("form,kind,told", FORMS_KINDS_TOLD, indirect=["told"])
+@pytest.mark.parametrize("far,sign", [(10, 1), (40, 1), (200, 1), (10, -1)])
+@pytest.mark.parametrize("hidden,prefix,ext", [(40, 90, 3), (1, 0, 5), (700, 1500, 2), (32, 32, 1)])
+def test_infinite_rotary_values(pa, gpu_device, form, kind, far, sign, hidden, prefix, ext, told):
+    """The first `hidden` keys have scores of -infinity (or +infinity) from a rotary value, those behind them scores 2^-far below 0: they have no weight, and with
+    none left a row is NaN."""
+    b = Batch(gpu_device, [prefix, 70], [ext, 2], 4, 512, *KINDS[kind], seed=18)
+    if form == "expanded":
+        b.weights(128)
+    at = b.q.shape[2] - P
+    b.q[..., :at] = b.q[..., :at] * 0.1
+    b.q[..., at] = 1
+    b.q[..., at + 1] = 8
+    b.rows_pool[:, 512:] = 0
+    b.c[:, 512:] = 0
+    keys = [b.rows_pool[s] for s in b.slots[0]] + [b.c[i] for i in range(ext)]
+    for i, key in enumerate(keys):
+        key[512] = sign * -float("inf") if i < hidden else 0
+        key[513] = -far * 0.6931471805599453 / (8 * b.scale)
+    b.fill(pa)
+    out = (b.absorbed if form == "absorbed" else b.expanded)(pa)
+    check_with_infinities(out, *definition_with_infinities(b, form), f"{far}, {sign}, {kind}")
