@@ -821,6 +821,7 @@ static ExpandLayout expand_layout(int B, int64_t T, int64_t max_kv_len, int H, i
     const int64_t listed = static_cast<int64_t>(B) * max_kv_len;
     l.cached_cap = listed < num_slots ? listed : num_slots;
     l.rows_cap = (T + l.cached_cap + kBlockRows - 1) / kBlockRows * kBlockRows;
+    if (l.rows_cap == 0) l.rows_cap = kBlockRows;  // (an empty batch has a size too)
     const size_t head_bytes = static_cast<size_t>(l.rows_cap) * N * 4;
     const int most = static_cast<int>(kExpandedBytes / head_bytes < 1 ? 1 : kExpandedBytes / head_bytes > static_cast<size_t>(H) ? H : kExpandedBytes / head_bytes);
     const int groups = (H + most - 1) / most;

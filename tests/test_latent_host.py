@@ -123,3 +123,16 @@ def test_the_stored_format_against_a_search_over_all_codes():
         best = d.amin(1, keepdim=True)
         code = torch.where(d == best, torch.arange(127)[None] % 2 * 1000 + torch.arange(127)[None], torch.tensor(10 ** 6)).amin(1) % 1000
         assert torch.equal(values, table[code] * 2.0 ** want_k * torch.sign(row).double())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16])
+@pytest.mark.parametrize("B,T,most", [(0, 0, 0), (0, 0, 100), (1, 0, 0), (3, 0, 10), (0, 5, 0)])
+def test_empty_batches_have_a_workspace_size(pa, dtype, B, T, most):
+    """(0 would mean that the arguments are invalid.)  In a process of its own, which a fault on the host would end."""
+    import subprocess
+    import sys
+    code = ("import torch\nfrom paper_2407_00023_amd import binding as pa\n"
+            f"a, b = pa.latent_workspace_bytes({B}, {T}, {most}, 16, 512, 64, {dtype}), pa.latent_expanded_workspace_bytes({B}, {T}, {most}, 16, 512, 64, 128, 4096, {dtype})\n"
+            "assert a > 0 and b > 0")
+    run = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True)
+    assert run.returncode == 0, run.stderr[-300:]
