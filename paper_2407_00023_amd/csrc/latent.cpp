@@ -69,8 +69,9 @@ extern "C" int pa_latent_attention(const void* q_ext, const void* c_ext, const v
 
 extern "C" size_t pa_latent_expanded_workspace_bytes(int B, int64_t T, int64_t max_kv_len, int H, int R, int P, int N, int64_t num_slots, int dtype) {
     if (!pa::sizes_ok(B, T, max_kv_len, H, R, P, dtype) || (N != 64 && N != 128) || num_slots <= 0 || num_slots > INT32_MAX) return 0;
-    const size_t n = dtype == PA_F32 ? pa::latent_expanded_f32_bytes(T, H, R) : pa::latent_expanded_bytes(B, T, max_kv_len, H, R, N, num_slots);
-    return n == 0 || n >= 256 ? n : 256;
+    if (dtype != PA_F32) return pa::latent_expanded_bytes(B, T, max_kv_len, H, R, N, num_slots);  // (0: too many rows)
+    const size_t n = pa::latent_expanded_f32_bytes(T, H, R);
+    return n > 256 ? n : 256;  // (an empty batch needs none; 0 means invalid)
 }
 
 extern "C" int pa_latent_attention_expanded(const void* q_ext, const void* c_ext, const void* w_k, const void* w_v, const void* latent_pool,

@@ -14,7 +14,7 @@ def pa(gpu_device):
     return binding
 
 
-@pytest.mark.parametrize("kind", ["bf16", "bf16_kv8"])
+@pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("form", ["absorbed", "expanded"])
 @pytest.mark.parametrize("prefix,ext", [([], []), ([5, 3], [0, 0])])
 def test_empty_batches(pa, gpu_device, form, kind, prefix, ext):

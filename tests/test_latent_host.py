@@ -125,14 +125,14 @@ def test_the_stored_format_against_a_search_over_all_codes():
         assert torch.equal(values, table[code] * 2.0 ** want_k * torch.sign(row).double())
 
 
-@pytest.mark.parametrize("dtype", [torch.bfloat16])
-@pytest.mark.parametrize("B,T,most", [(0, 0, 0), (0, 0, 100), (1, 0, 0), (3, 0, 10), (0, 5, 0)])
-def test_empty_batches_have_a_workspace_size(pa, dtype, B, T, most):
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_empty_batches_have_a_workspace_size(pa, dtype):
     """(0 would mean that the arguments are invalid.)  In a process of its own, which a fault on the host would end."""
     import subprocess
     import sys
     code = ("import torch\nfrom paper_2407_00023_amd import binding as pa\n"
-            f"a, b = pa.latent_workspace_bytes({B}, {T}, {most}, 16, 512, 64, {dtype}), pa.latent_expanded_workspace_bytes({B}, {T}, {most}, 16, 512, 64, 128, 4096, {dtype})\n"
-            "assert a > 0 and b > 0")
+            "for B, T, most in [(0, 0, 0), (0, 0, 100), (1, 0, 0), (3, 0, 10), (0, 5, 0)]:\n"
+            f"    assert pa.latent_workspace_bytes(B, T, most, 16, 512, 64, {dtype}) > 0\n"
+            f"    assert pa.latent_expanded_workspace_bytes(B, T, most, 16, 512, 64, 128, 4096, {dtype}) > 0")
     run = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True)
     assert run.returncode == 0, run.stderr[-300:]
