@@ -822,7 +822,7 @@ static ExpandLayout expand_layout(int B, int64_t T, int64_t max_kv_len, int H, i
     l.cached_cap = listed < num_slots ? listed : num_slots;
     l.rows_cap = (T + l.cached_cap + kBlockRows - 1) / kBlockRows * kBlockRows;
     if (l.rows_cap == 0) l.rows_cap = kBlockRows;  // (an empty batch has a size too)
-    const size_t head_bytes = static_cast<size_t>(l.rows_cap) * N * 4;
+    const size_t head_bytes = static_cast<size_t>(l.rows_cap) * (N * 4 + 2);  // keys, values, exponents
     const int most = static_cast<int>(kExpandedBytes / head_bytes < 1 ? 1 : kExpandedBytes / head_bytes > static_cast<size_t>(H) ? H : kExpandedBytes / head_bytes);
     const int groups = (H + most - 1) / most;
     l.heads = (H + groups - 1) / groups;
@@ -838,10 +838,14 @@ static ExpandLayout expand_layout(int B, int64_t T, int64_t max_kv_len, int H, i
     l.row_of = take(sizeof(int32_t) * (listed + 1));
     l.a = take(static_cast<size_t>(l.rows_cap) * R * 2);
     l.rope = take(static_cast<size_t>(l.rows_cap) * kRope * 2);
-    l.k_exp = take(static_cast<size_t>(l.heads) * l.rows_cap);
-    l.v_exp = take(static_cast<size_t>(l.heads) * l.rows_cap);
-    l.k = take(static_cast<size_t>(l.heads) * l.rows_cap * N * 2);
-    l.v = take(static_cast<size_t>(l.heads) * l.rows_cap * N * 2);
+    // Room for all heads, or kExpandedBytes of it, or one: it does not fall when a batch grows, as what the heads at once take does where it holds one less, so that
+    // a workspace is enough for every smaller batch.
+    const size_t all = head_bytes * H, room = all <= kExpandedBytes ? all : head_bytes > kExpandedBytes ? head_bytes : kExpandedBytes;
+    const size_t exps = static_cast<size_t>(l.heads) * l.rows_cap, values = exps * N * 2;
+    l.k = take(room);
+    l.v = l.k + values;
+    l.k_exp = l.v + values;
+    l.v_exp = l.k_exp + exps;
     l.parts = take(latent_parts_layout(kExpWorkgroups, kExpM, N).total);
     l.total = at;
     return l;

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from latent_side import Batch, P
+from latent_side import Batch, P, check
 
 pytestmark = pytest.mark.gpu
 KINDS = {"f32": (torch.float32, False), "bf16": (torch.bfloat16, False), "bf16_kv8": (torch.bfloat16, True)}
@@ -31,3 +31,16 @@ def test_empty_batches(pa, gpu_device, form, kind, prefix, ext):
     none = torch.zeros(0, dtype=torch.int32, device=gpu_device)
     pa.append_latent(b.pool, none, b.c, rope_dim=P, **b.kw)
     assert tuple(pa.gather_latent(b.pool, none, latent_dim=512, rope_dim=P, dtype=b.dtype, **b.kw).shape) == (0, 576)
+
+
+@pytest.mark.parametrize("most,less", [(8200, 7800), (9000, 8100)])
+def test_a_workspace_sized_once(pa, gpu_device, most, less):
+    """Sized for the largest batch, used for a smaller one that holds more heads at once."""
+    H, slots = 128, 1 << 17
+    size = pa.latent_expanded_workspace_bytes(8, 512, most, H, 512, P, 128, slots, torch.bfloat16)
+    b = Batch(gpu_device, [less - 2] + [200] * 7, [2] * 8, H, 512, num_slots=slots, seed=2).fill(pa).weights(128)
+    assert b.max_kv_len == less
+    out = b.expanded(pa, workspace=torch.empty(size, dtype=torch.uint8, device=gpu_device))
+    assert torch.equal(out.view(torch.int16), b.expanded(pa).view(torch.int16))
+    ref, bound = b.reference("expanded")
+    check(out, ref, bound, f"{less} of {most}")

@@ -136,3 +136,27 @@ def test_empty_batches_have_a_workspace_size(pa, dtype):
             f"    assert pa.latent_expanded_workspace_bytes(B, T, most, 16, 512, 64, 128, 4096, {dtype}) > 0")
     run = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True)
     assert run.returncode == 0, run.stderr[-300:]
+
+
+@pytest.mark.parametrize("form", ["absorbed", "expanded"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("H,R,N", [(1, 256, 64), (16, 512, 128), (32, 512, 128), (128, 512, 128), (130, 256, 64)])
+def test_a_workspace_is_enough_for_smaller_batches(pa, form, dtype, H, R, N):
+    """Sizes do not fall when B, T or max_kv_len rises, across the places where the expanded form holds fewer heads at once."""
+    def size(B, T, most):
+        if form == "absorbed":
+            return pa.latent_workspace_bytes(B, T, most, H, R, 64, dtype)
+        return pa.latent_expanded_workspace_bytes(B, T, most, H, R, 64, N, 1 << 20, dtype)
+
+    of_T = [0, 1, 2, 3, 31, 32, 33, 64, 65, 500, 512, 2048, 2112, 5000, 8192, 30000, 60000]
+    of_most = [1, 31, 32, 100, 1000, 2000, 4000, 7800, 8100, 8200, 16000, 16500, 33000, 65000, 70000, 131072, 260096]
+    for B in [1, 2, 3, 8, 100]:
+        sizes = [[size(B, T, most) for most in of_most] for T in of_T]
+        for row, below in zip(sizes, sizes[1:] + [None]):
+            assert row == sorted(row), (B, row)
+            if below:
+                assert all(x <= y for x, y in zip(row, below)), (B, row, below)
+    for T in of_T:
+        for most in of_most:
+            sizes = [size(B, T, most) for B in [0, 1, 2, 3, 4, 7, 8, 9, 16, 17, 100, 1000]]
+            assert sizes == sorted(sizes), (T, most, sizes)
