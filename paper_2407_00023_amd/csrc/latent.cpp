@@ -8,7 +8,7 @@ int latent_attention_f32(const void* q, const LatentBatch& b, int H, int R, floa
 int latent_expanded_f32(const void* q, const LatentBatch& b, const void* w_k, const void* w_v, int H, int R, int N, float scale, void* out, void* scratch,
                         hipStream_t stream);
 size_t latent_expanded_f32_bytes(int64_t T, int H, int R);
-size_t latent_workspace_bytes_bf16(int B, int64_t T, int64_t max_kv_len, int H, int R);
+size_t latent_workspace_bytes_bf16(int64_t T, int H, int R);
 int latent_attention_bf16(const void* q, const LatentBatch& b, int64_t max_kv_len, int H, int R, bool kv8, float scale, void* out, void* workspace,
                           hipStream_t stream);
 size_t latent_expanded_bytes(int B, int64_t T, int64_t max_kv_len, int H, int R, int N, int64_t num_slots);
@@ -49,7 +49,7 @@ static int check(const char* fn, const void* q, const LatentBatch& b, int64_t ma
 
 extern "C" size_t pa_latent_workspace_bytes(int B, int64_t T, int64_t max_kv_len, int H, int R, int P, int dtype) {
     if (!pa::sizes_ok(B, T, max_kv_len, H, R, P, dtype)) return 0;
-    return dtype == PA_F32 ? 256 : pa::latent_workspace_bytes_bf16(B, T, max_kv_len, H, R);  // (fp32 needs none; 0 means invalid)
+    return dtype == PA_F32 ? 256 : pa::latent_workspace_bytes_bf16(T, H, R);  // (fp32 needs none; 0 means invalid)
 }
 
 extern "C" int pa_latent_attention(const void* q_ext, const void* c_ext, const void* latent_pool, const int32_t* slot_idx,

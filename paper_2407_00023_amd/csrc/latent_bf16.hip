@@ -632,9 +632,10 @@ static int tile_rows(int B, int64_t T, int64_t max_kv_len, int H) {
     return keys <= 128 ? 32 : keys <= 1024 && most > 64 ? 64 : most;
 }
 
-size_t latent_workspace_bytes_bf16(int B, int64_t T, int64_t max_kv_len, int H, int R) {
-    (void)B, (void)T, (void)max_kv_len, (void)H;
-    return latent_parts_layout(kWorkgroups, 128, R).total;  // (good for every batch)
+// (parts of tiles as large as these rows fill in one request: fewer requests than there are may take larger ones, more keys too)
+size_t latent_workspace_bytes_bf16(int64_t T, int H, int R) {
+    const int64_t rows = T * H;
+    return latent_parts_layout(kWorkgroups, rows <= 32 ? 32 : rows <= 64 ? 64 : 128, R).total;
 }
 
 template <int R, int M, bool KV8>

@@ -160,3 +160,10 @@ def test_a_workspace_is_enough_for_smaller_batches(pa, form, dtype, H, R, N):
         for most in of_most:
             sizes = [size(B, T, most) for B in [0, 1, 2, 3, 4, 7, 8, 9, 16, 17, 100, 1000]]
             assert sizes == sorted(sizes), (T, most, sizes)
+
+
+def test_the_absorbed_forms_workspace_goes_by_its_tiles(pa):
+    """Partial results of 256 workgroups, three tiles each, of 32 rows where a call has no more, of 128 at most."""
+    size = lambda T, most, H: pa.latent_workspace_bytes(1, T, most, H, 512, 64, torch.bfloat16) / (3 * 256 * 512 * 4)
+    assert 32 <= size(1, 2133, 16) < 33 and 32 <= size(2, 10 ** 6, 16) < 33
+    assert 64 <= size(4, 10 ** 6, 16) < 65 and 128 <= size(128, 7800, 128) < 129
