@@ -480,7 +480,7 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
             const int k = exponent_of(top), alone = min(exponent_of(top_n), k), k_n = is_scaled ? alone : k;
             const float by = power_of_two(-k), by_n = power_of_two(-k_n);
             q_exp[rb] = k_n - k;
-            c[rb] = scale_log2e * power_of_two(k);
+            c[rb] = fmaxf(scale_log2e * power_of_two(k), 1.401298464324817e-45f);  // (never 0, which would make NaN of a hidden key's -infinity)
 #pragma unroll
             for (int s = 0; s < KS + KSR; ++s) {
                 const unsigned w[4] = {raw[s].x, raw[s].y, raw[s].z, raw[s].w};

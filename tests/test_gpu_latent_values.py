@@ -319,3 +319,16 @@ def test_infinite_rotary_values(pa, gpu_device, form, kind, far, sign, hidden, p
     b.fill(pa)
     out = (b.absorbed if form == "absorbed" else b.expanded)(pa)
     check_with_infinities(out, *definition_with_infinities(b, form), f"{far}, {sign}, {kind}")
+
+
+# ---- the ends of the range -----------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("form", ["absorbed", "expanded"])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("of_q,of_scale", [(-118, -30), (-100, -40), (-10, -100), (100, -140)])
+def test_queries_and_scales_so_small_that_all_keys_weigh_the_same(pa, gpu_device, form, kind, of_q, of_scale):
+    b = Batch(gpu_device, [300, 5], [3, 40], 4, 512, *KINDS[kind], seed=19).fill(pa)
+    if form == "expanded":
+        b.weights(128)
+    b.q, b.scale = b.q * 2.0 ** of_q, 2.0 ** of_scale
+    check((b.absorbed if form == "absorbed" else b.expanded)(pa), *b.reference(form), f"2^{of_q}, scale 2^{of_scale}, {kind}")
