@@ -423,12 +423,12 @@ size_t pa_latent_workspace_bytes(int B, int64_t T, int64_t max_kv_len, int H, in
  * out   [T, H, R]       latent_pool as written by pa_append_latent with the same R, P, num_slots, dtype
  * The other arguments, what happens to slots outside the pool, to requests without extend tokens and
  * to a batch on the device larger than T says (pa_extend_status, bf16) are as for pa_extend_attention;
- * scale has to be positive and finite, and scores within fp32, also times log2(e).  A latent value
- * that is infinite or NaN makes NaN what sees it, as the formula has it (its column; every column
- * unless its key's score is -infinity), and nothing else.  workspace: at least
- * pa_latent_workspace_bytes(...), 256-byte aligned, whatever it holds; calls that overlap in time must
- * not share one.  bf16: probabilities are rounded to bf16 before they are multiplied with the rows.
- * B at most 65,536. */
+ * scale has to be positive and finite, scores within fp32, also times log2(e), and finite latent
+ * values within 2^64 (bf16: sums are fp32, with weights of up to 2^40 a key; the probabilities are
+ * rounded to bf16 before they are multiplied with the rows).  A latent value that is infinite or NaN
+ * makes NaN what sees it, as the formula has it (its column; every column unless its key's score is
+ * -infinity), and nothing else.  workspace: at least pa_latent_workspace_bytes(...), 256-byte aligned,
+ * whatever it holds; calls that overlap in time must not share one.  B at most 65,536. */
 int pa_latent_attention(const void* q_ext, const void* c_ext, const void* latent_pool, const int32_t* slot_idx,
                         const int32_t* slot_offsets, const int32_t* prefix_len, const int32_t* ext_len,
                         const int32_t* ext_offsets, int B, int64_t T, int64_t max_kv_len, int H, int R, int P,

@@ -22,9 +22,10 @@
 // probability may be as large as kMost, which fp32 and bf16 hold as exactly as 1.  Against maxima so large that their rounding shows (moved_maximum()) those of the
 // settlement itself are held to 2^kCap; the step counts as done then.
 //
-// Measured: 64 heads, 16 requests of 20 to 80 new tokens over 4 documents of 16 384 rows (1.9 TFLOP): 1850 us, 1.05 PFLOP/s, where a plain product of 16 384
-// squared reaches 1.39; bound by LDS and by waiting beside the matrix cores, which are busy 45 % of the cycles.  128 heads, 128 requests of one token, 500 to 7800 keys: 257 us.
-// 16 heads, 48 requests, 2000 to 24 000 keys of the 8-bit pool: 176 us, 2.7 TB/s, bound by what a step does outside its products, most of it turning codes into bf16.
+// Measured: 64 heads, 16 requests of 20 to 80 new tokens over 4 documents of 16 384 rows (1.9 TFLOP): 1800 us, 1.05 PFLOP/s, where a plain product of 16 384
+// squared reaches 1.39; the matrix cores are busy 45 % of the cycles, LDS 23 %, a wave waits a quarter of its own: none is full, but there is one wave on a SIMD, and
+// nothing beside it while it waits.  128 heads, 128 requests of one token, 500 to 7800 keys: 258 us (27 %, 14 %, 39 %).
+// 16 heads, 48 requests, 2000 to 24 000 keys of the 8-bit pool: 172 us, 2.7 TB/s, bound by what a step does outside its products, most of it turning codes into bf16.
 //
 // LDS is swizzled in pieces of 16 bytes (swz()) so that reading 16 bytes down 16 rows and the transposing reads of 8 bytes across 8 rows are both
 // free of bank conflicts; direct loads write 1 KB of consecutive LDS, so the swizzle is applied to the address in memory.
@@ -372,6 +373,8 @@ __global__ __launch_bounds__(256, 1) void latent_bf16_kernel(const __hip_bfloat1
             }
         };
         // a piece of the probabilities of the scores against the maxima as they stand, into buffer rel % 2; their sums
+        // (Rounded to bf16, since a matrix instruction takes one type and the rows are bf16: a result is 1.7e-3 to 2.4e-3 off, relatively, of which 1.7e-3 is the rounding of
+        // the result itself.  A second product with what the rounding left would cost as much as the first.)
         float sum[RW];
         auto probabilities = [&](int rel, int kb, int rb, auto moved) __attribute__((always_inline)) {
             float p[4];

@@ -10,9 +10,10 @@
 // Expanded keys and values lie in the workspace for as many heads at a time as fit kExpandedBytes.
 //
 // Measured: 24 requests of 200 to 1000 new tokens over 4 documents, 32 heads, R = 512, N = 128 (21 400 rows; 0.9 TFLOP): mark and collect 25 us, expand 200 us,
-// attend 1100 us, join 30 us.  The expansion writes 350 MB and multiplies 180 GFLOP (0.9 PFLOP/s): bound by its stores beside the matrix cores, which are busy
-// 47 % of the cycles.  The attention is bound by LDS, of which every wave reads all keys and values for 32 rows of q: 74 % of its cycles, the matrix cores 38 %.
-// (Waves of 64 rows, one to a SIMD, halve these reads and take longer, 1320 us, since nothing is beside a wave that waits.)
+// attend 1000 us, join 30 us.  The expansion writes 350 MB and multiplies 180 GFLOP (0.9 PFLOP/s): bound by its stores beside the matrix cores, which are busy
+// 50 % of the cycles.  In the attention these are busy 38 % of the cycles and LDS 22 %; a wave waits 29 % of its own, and 5.7 GB come past the L2s, 16 times the
+// keys and values that there are, since a tile of 128 rows of q reads all of its head's.  (Waves of 64 rows, one to a SIMD, halve the LDS reads and take longer,
+// 1320 us, since nothing is beside a wave that waits.)  The branch `scaled` (below) takes a quarter to a third longer: 1360 us.
 //
 // fp16 and not bf16, because a rounding of keys, one of values and one of probabilities would each cost as much as the result's own: with 11
 // bits they are an eighth of it each.  What fp16 lacks in range is made up for: a row of K or V of a head whose largest value is out of

@@ -92,6 +92,14 @@ def test_expanded_rows_of_no_request_may_hold_anything(pa, gpu_device, kind, val
     assert torch.equal(bits(got), bits(alone)) and bool((out[[0, 1, 5, 10, 16]] == 9.0).all())
 
 
+def test_expanded_heads_of_different_sizes_in_several_groups(pa, gpu_device):
+    """Keys and values of all heads take more than the workspace holds at a time; some heads of each group have values of powers of their own."""
+    b = Batch(gpu_device, [70000], [2], 130, 512, seed=2).fill(pa).weights(128)
+    b.w_v[::3] = b.w_v[::3] * 2.0 ** -12
+    b.w_k[1::7] = b.w_k[1::7] * 2.0 ** -14
+    check(b.expanded(pa), *b.reference("expanded"), "130 heads")
+
+
 # ---- scores --------------------------------------------------------------------------------------------------------------------
 
 def check_winners(b, out, form):
