@@ -769,8 +769,10 @@ __global__ __launch_bounds__(256, 2) void latent_expanded_kernel(const __hip_bfl
                 const float sum = row_sum(l[rb]);
                 const int row = wrow + 16 * rb + n;
                 if (row >= rows_here) continue;
-                if (!whole && g4 == 0) parts.ml[static_cast<size_t>(part) * kExpM + row] = make_float2(m[rb], sum);
-                const float inv = whole ? 1.f / sum : 1.f;
+                // (values so large that a part's sum of them could be more than fp32 holds: their mean instead, with the weight in the maximum)
+                const bool mean = !whole && scaled && d[rb] > 64.f && sum > 0.f;
+                if (!whole && g4 == 0) parts.ml[static_cast<size_t>(part) * kExpM + row] = mean ? make_float2(m[rb] + __builtin_amdgcn_logf(sum), 1.f) : make_float2(m[rb], sum);
+                const float inv = whole || mean ? 1.f / sum : 1.f;
 #pragma unroll
                 for (int cb = 0; cb < NB; ++cb) {
                     f32x4 y = o[rb][cb];

@@ -92,6 +92,16 @@ def test_expanded_rows_of_no_request_may_hold_anything(pa, gpu_device, kind, val
     assert torch.equal(bits(got), bits(alone)) and bool((out[[0, 1, 5, 10, 16]] == 9.0).all())
 
 
+@pytest.mark.parametrize("kind", ["bf16", "bf16_kv8"])
+@pytest.mark.parametrize("prefix,ext", [([6000], [2]), ([200], [2]), ([40000, 300], [3, 130])])
+@pytest.mark.parametrize("of", [90, 112, 120, -100])
+def test_expanded_values_at_the_ends_of_the_range(pa, gpu_device, kind, of, prefix, ext):
+    """Results of up to 2^120, from whole tiles and from tiles in parts: no sum on the way is larger than fp32 holds."""
+    b = Batch(gpu_device, prefix, ext, 2, 512, *KINDS[kind], seed=20).fill(pa).weights(128)
+    b.w_v = b.w_v * 2.0 ** of
+    check(b.expanded(pa), *b.reference("expanded"), f"2^{of}, {kind}")
+
+
 def test_expanded_heads_of_different_sizes_in_several_groups(pa, gpu_device):
     """Keys and values of all heads take more than the workspace holds at a time; some heads of each group have values of powers of their own."""
     b = Batch(gpu_device, [70000], [2], 130, 512, seed=2).fill(pa).weights(128)
